@@ -147,6 +147,83 @@ int osprey_kv_append(const osprey_ctx *ctx, const osprey_kv *kv, int B, const in
                      int64_t total_rows, const void *k_rows, const void *v_rows,
                      int32_t *dev_status, void *stream);
 
+/* osprey_kv_append with unrotated keys: k_rows are turned to their positions
+ * (rotate-half at rope_theta, as the draft step turns its own) on the way into
+ * the pages, in float32 with exact angles, and rounded once to bf16.
+ *   rows_dtype  OSPREY_BF16 or OSPREY_F32, of k_rows and v_rows
+ *   row_stride  elements between one row and the next (at least
+ *          n_kv_heads * head_dim; 0: just that), so that rows can be read where
+ *          a fused QKV projection left them; a row is [n_kv_heads][head_dim] and
+ *          layer l starts total_rows * row_stride elements after layer l - 1.
+ *          Rows start on 16 bytes.
+ *   layer  -1: rows of every layer; l in [0, n_layers): of that layer alone (a
+ *          model that appends as it goes from layer to layer)
+ *   advance  1: seq_len[b] += n_rows[b] after the rows are written; 0: lengths
+ *          stay as they are (all layers of a step but the last)
+ * Host and device errors as osprey_kv_append; a sequence whose rows do not all
+ * fit, or with a page id out of range among them, is left untouched. */
+int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv, int layer, int B, const int32_t *n_rows,
+                          int64_t total_rows, const void *k_rows, const void *v_rows, int rows_dtype,
+                          int64_t row_stride, int advance, int32_t *dev_status, void *stream);
+
+/* Paged KV cache in 8 bits (device, caller-owned).  A page of 16 positions of one
+ * KV head is a block with one scale each for K and V.  A block is rounded to 8
+ * bits once, when its last position is written; the rows of the unfinished page
+ * (and of the last tail_pages pages, the unfinished one among them) are held in
+ * bf16 in a ring, the tail.  Positions below 16 * floor(length / 16) are read in
+ * 8 bits, the rest from the tail.
+ *   k8, v8  [n_layers][n_pages][n_kv_heads][16 * head_dim] e4m3 codes x / scale.
+ *           K: code of (slot t, dim d) at ((t / 8) * (head_dim / 16) + d / 16) *
+ *           128 + (t % 8) * 16 + d % 16; V: at d * 16 + t.  Codes are finite.
+ *   k_scale, v_scale [n_layers][n_pages][n_kv_heads] float.  As written here: the
+ *           smallest power of two, at least 2^-100, with max |x| <= 448 scale; NaN
+ *           (and codes 0) for a block with a value that is not finite, so that
+ *           every output that sees a key of the block is NaN.  Attention takes any
+ *           positive scale.
+ *   k_tail, v_tail [n_layers][B][tail_pages][n_kv_heads][16][head_dim] bf16:
+ *           position t of sequence b in ring page (t / 16) % tail_pages, slot t % 16
+ *   page_table, seq_len, max_pages_per_seq, n_pages as osprey_kv
+ *   tail_pages >= 1.  A caller may take back the last 16 * (tail_pages - 1)
+ *           positions of a sequence by lowering seq_len: their page's rows are
+ *           still in the tail. */
+typedef struct osprey_kv8 {
+    void *k8, *v8;
+    float *k_scale, *v_scale;
+    void *k_tail, *v_tail;
+    int32_t *page_table, *seq_len;
+    int32_t max_pages_per_seq, n_pages, tail_pages;
+} osprey_kv8;
+
+/* osprey_kv_append_rope into the 8-bit cache (rotate 0: keys are rotated already).
+ * Arguments and errors as there. */
+int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, int B, const int32_t *n_rows,
+                      int64_t total_rows, const void *k_rows, const void *v_rows, int rows_dtype,
+                      int64_t row_stride, int rotate, int advance, int32_t *dev_status, void *stream);
+
+/* Causal attention of each sequence's newest rows over the 8-bit cache, one
+ * layer:  out = softmax(q K^T / sqrt(head_dim)) V, query head h on KV head
+ * h / (n_q_heads / n_kv_heads).
+ *   n_rows [B] int32 (device), 0 <= n_rows[b] <= max_rows: row j of sequence b is
+ *          position T - n_rows[b] + j and sees the positions up to its own, T =
+ *          seq_len[b] (advanced 1) or seq_len[b] + n_rows[b] (advanced 0: the
+ *          rows are appended, the length is not).  Their K/V rows are in the cache.
+ *   max_rows 1 .. 64
+ *   q [B][max_rows] rows of [n_q_heads][head_dim], q_stride elements apart (0:
+ *          dense), OSPREY_BF16 or OSPREY_F32; rotate 1: turned to their positions
+ *          on the way.  Rows start on 16 bytes.
+ *   out [B][max_rows][n_q_heads][head_dim] of q's type, 16-byte aligned; rows from
+ *          n_rows[b] on are left as they were
+ * Sums and softmax statistics are float32; q and the weights enter the tensor
+ * cores as e4m3 planes that keep 8 (q) and 12 to 16 (weights) significant bits of
+ * bf16 calls, 24 of float32 ones.  No workspace.
+ * Device errors: INVALID_ARG (n_rows[b] outside 0 .. max_rows, or more than T),
+ * CAPACITY (T past the page table, a page id out of range); such a sequence's
+ * output rows are 0.
+ * Host errors: INVALID_ARG, DTYPE. */
+int osprey_kv8_attend(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, int B, int max_rows,
+                      const int32_t *n_rows, const void *q, int dtype, int64_t q_stride, int rotate, int advanced,
+                      void *out, int32_t *dev_status, void *stream);
+
 /* One draft call: extend, then a K-token chain (Sec. 3.1, Eq. 1-3, Sec. 3.4).
  *   n_new  [B] int32 (device), 1 <= n_new[b] <= max_new: extend rows of b
  *   tokens [B][max_new] int32: extend row j is token tokens[b][j] at position

@@ -62,6 +62,11 @@ class osprey_kv(ctypes.Structure):
                 ("max_pages_per_seq", _i32), ("n_pages", _i32)]
 
 
+class osprey_kv8(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("k8", "v8", "k_scale", "v_scale", "k_tail", "v_tail", "page_table", "seq_len")] + \
+               [("max_pages_per_seq", _i32), ("n_pages", _i32), ("tail_pages", _i32)]
+
+
 def _sig(name, res, args):
     f = getattr(_lib, name)
     f.restype, f.argtypes = res, args
@@ -75,6 +80,15 @@ _c_destroy = _sig("osprey_destroy", None, [_vp])
 _c_draft_ws = _sig("osprey_draft_workspace_bytes", _sz, [_vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int])
 _c_kv_append = _sig("osprey_kv_append", ctypes.c_int, [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, _vp, _i64,
                                                         _vp, _vp, _vp, _vp])
+_c_kv_append_rope = _sig("osprey_kv_append_rope", ctypes.c_int,
+                         [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, ctypes.c_int, _vp, _i64, _vp, _vp, ctypes.c_int,
+                          _i64, ctypes.c_int, _vp, _vp])
+_c_kv8_append = _sig("osprey_kv8_append", ctypes.c_int,
+                     [_vp, ctypes.POINTER(osprey_kv8), ctypes.c_int, ctypes.c_int, _vp, _i64, _vp, _vp, ctypes.c_int,
+                      _i64, ctypes.c_int, ctypes.c_int, _vp, _vp])
+_c_kv8_attend = _sig("osprey_kv8_attend", ctypes.c_int,
+                     [_vp, ctypes.POINTER(osprey_kv8), ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, ctypes.c_int,
+                      _i64, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp])
 _c_draft = _sig("osprey_draft_step", ctypes.c_int,
                 [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _f32, _vp,
                  _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp])
@@ -109,7 +123,7 @@ _c_launch_count = _sig("osprey_launch_count", _i64, [])
 _c_selftest_wait = _sig("osprey_selftest_wait_timeout", ctypes.c_int, [_i64, _vp, _vp])
 
 EXPORTED = ["osprey_last_error", "osprey_create", "osprey_destroy", "osprey_draft_workspace_bytes",
-            "osprey_kv_append", "osprey_draft_step", "osprey_draft_step_hidden", "osprey_draft_step_topk",
+            "osprey_kv_append", "osprey_kv_append_rope", "osprey_kv8_append", "osprey_kv8_attend", "osprey_draft_step", "osprey_draft_step_hidden", "osprey_draft_step_topk",
             "osprey_verify_tree", "osprey_dflash_workspace_bytes",
             "osprey_dflash_step", "osprey_verify_workspace_bytes",
             "osprey_verify", "osprey_verify_static", "osprey_verify_hidden_workspace_bytes", "osprey_verify_hidden",
@@ -233,6 +247,57 @@ def alloc_kv(shape: DrafterShape, page_table: np.ndarray, n_pages: int, device="
                    torch.zeros(B, dtype=torch.int32, device=device))
 
 
+@dataclass
+class Kv8Cache:
+    """The 8-bit paged cache: codes and scales of finished pages, a bf16 ring for the last ones (include/osprey.h)."""
+    k8: torch.Tensor           # [L, n_pages, Hkv, 16 * hd] uint8 (e4m3 codes)
+    v8: torch.Tensor
+    k_scale: torch.Tensor      # [L, n_pages, Hkv] float32
+    v_scale: torch.Tensor
+    k_tail: torch.Tensor       # [L, B * tail_pages, Hkv, 16, hd] bf16
+    v_tail: torch.Tensor
+    page_table: torch.Tensor   # [B, max_pages] int32
+    seq_len: torch.Tensor      # [B] int32
+
+    @property
+    def max_pages(self) -> int:
+        return self.page_table.shape[1]
+
+    @property
+    def n_pages(self) -> int:
+        return self.k8.shape[1]
+
+    @property
+    def tail_pages(self) -> int:
+        return self.k_tail.shape[1] // self.page_table.shape[0]
+
+    def c_struct(self, shape: DrafterShape) -> osprey_kv8:
+        """The C struct, after the checks of the tensors against the drafter's shape."""
+        L, H, hd = shape.n_layers, shape.n_kv_heads, shape.head_dim
+        B, n, t = self.page_table.shape[0], self.n_pages, self.tail_pages
+        _need(self.k8, torch.uint8, (L, n, H, 16 * hd), "k8")
+        _need(self.v8, torch.uint8, (L, n, H, 16 * hd), "v8")
+        _need(self.k_scale, torch.float32, (L, n, H), "k_scale")
+        _need(self.v_scale, torch.float32, (L, n, H), "v_scale")
+        _need(self.k_tail, torch.bfloat16, (L, B * t, H, 16, hd), "k_tail")
+        _need(self.v_tail, torch.bfloat16, (L, B * t, H, 16, hd), "v_tail")
+        _need(self.page_table, torch.int32, None, "page_table")
+        _need(self.seq_len, torch.int32, (B,), "seq_len")
+        return osprey_kv8(self.k8.data_ptr(), self.v8.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                          self.k_tail.data_ptr(), self.v_tail.data_ptr(), self.page_table.data_ptr(),
+                          self.seq_len.data_ptr(), self.max_pages, n, t)
+
+
+def alloc_kv8(shape: DrafterShape, page_table: np.ndarray, n_pages: int, tail_pages: int = 2, device="cuda") -> Kv8Cache:
+    B, L, H, hd = page_table.shape[0], shape.n_layers, shape.n_kv_heads, shape.head_dim
+    z = lambda dt, *s: torch.zeros(s, dtype=dt, device=device)  # noqa: E731
+    return Kv8Cache(z(torch.uint8, L, n_pages, H, 16 * hd), z(torch.uint8, L, n_pages, H, 16 * hd),
+                    torch.ones((L, n_pages, H), dtype=torch.float32, device=device),
+                    torch.ones((L, n_pages, H), dtype=torch.float32, device=device),
+                    z(torch.bfloat16, L, B * tail_pages, H, 16, hd), z(torch.bfloat16, L, B * tail_pages, H, 16, hd),
+                    torch.from_numpy(np.ascontiguousarray(page_table, np.int32)).to(device), z(torch.int32, B))
+
+
 def to_device_bf16(bits: np.ndarray, device="cuda") -> torch.Tensor:
     """bf16 bit patterns (uint16 numpy) -> a bf16 device tensor with the same bytes."""
     return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).view(torch.bfloat16).to(device)
@@ -263,6 +328,89 @@ def osprey_kv_append(ctx: Ctx, kv: KvCache, n_rows: torch.Tensor, k_rows: torch.
     kvs = kv.c_struct()
     _check(_c_kv_append(ctx.handle, ctypes.byref(kvs), B, _ptr(n_rows), total, _ptr(k_rows), _ptr(v_rows),
                         _ptr(status), _stream(stream)))
+
+
+_ROWS = {torch.bfloat16: OSPREY_BF16, torch.float32: OSPREY_F32}
+
+
+def _strided_rows(t, lead, inner, name):
+    """Checks rows [*lead, *inner] whose last two dimensions are dense; the distance between rows, in elements."""
+    if t.dtype not in _ROWS:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected bfloat16 or float32")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} must be on the current device")
+    if tuple(t.shape) != (*lead, *inner):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(*lead, *inner)}")
+    dense = inner[0] * inner[1]
+    if t.numel() == 0:
+        return dense
+    st = t.stride()
+    if (inner[1] > 1 and st[-1] != 1) or (inner[0] > 1 and st[-2] != inner[1]):
+        raise ValueError(f"{name}: a row must be dense")
+    row = st[len(lead) - 1] if lead[-1] > 1 else (st[0] if len(lead) > 1 and lead[0] > 1 else dense)
+    if row < dense or (len(lead) > 1 and lead[0] > 1 and st[0] != row * lead[1]):
+        raise ValueError(f"{name}: rows must be evenly spaced and not overlap")
+    return row
+
+
+def _append_rows(ctx, B, n_rows, k_rows, v_rows, status, layer):
+    s = ctx.shape
+    _need(n_rows, torch.int32, (B,), "n_rows")
+    _need(status, torch.int32, (1,), "status")
+    lead = tuple(k_rows.shape[:-2])
+    if len(lead) != (2 if layer is None else 1):
+        raise ValueError("rows are [n_layers, total, Hkv, hd], or [total, Hkv, hd] of one layer")
+    if layer is None and lead[0] != s.n_layers:
+        raise ValueError(f"k_rows: {lead[0]} layers, expected {s.n_layers}")
+    inner = (s.n_kv_heads, s.head_dim)
+    stride = _strided_rows(k_rows, lead, inner, "k_rows")
+    if _strided_rows(v_rows, lead, inner, "v_rows") != stride or v_rows.dtype != k_rows.dtype:
+        raise ValueError("k_rows and v_rows must have the same type and spacing")
+    return lead[-1], stride
+
+
+def osprey_kv_append_rope(ctx: Ctx, kv: KvCache, n_rows: torch.Tensor, k_rows: torch.Tensor, v_rows: torch.Tensor,
+                          status: torch.Tensor, layer: int | None = None, advance: bool = True, stream=None):
+    """osprey_kv_append of unrotated keys.  Rows [n_layers, total, Hkv, hd], or [total, Hkv, hd] of one layer, bf16 or
+    float32; rows may be views into a wider projection's output."""
+    B = kv.page_table.shape[0]
+    total, stride = _append_rows(ctx, B, n_rows, k_rows, v_rows, status, layer)
+    kvs = kv.c_struct()
+    _check(_c_kv_append_rope(ctx.handle, ctypes.byref(kvs), -1 if layer is None else layer, B, _ptr(n_rows), total,
+                             _ptr(k_rows), _ptr(v_rows), _ROWS[k_rows.dtype], stride, int(advance), _ptr(status),
+                             _stream(stream)))
+
+
+def osprey_kv8_append(ctx: Ctx, kv: Kv8Cache, n_rows: torch.Tensor, k_rows: torch.Tensor, v_rows: torch.Tensor,
+                      status: torch.Tensor, layer: int | None = None, rotate: bool = True, advance: bool = True,
+                      stream=None):
+    """Appends rows (as osprey_kv_append_rope takes them) to the 8-bit cache."""
+    B = kv.page_table.shape[0]
+    total, stride = _append_rows(ctx, B, n_rows, k_rows, v_rows, status, layer)
+    kvs = kv.c_struct(ctx.shape)
+    _check(_c_kv8_append(ctx.handle, ctypes.byref(kvs), -1 if layer is None else layer, B, _ptr(n_rows), total,
+                         _ptr(k_rows), _ptr(v_rows), _ROWS[k_rows.dtype], stride, int(rotate), int(advance),
+                         _ptr(status), _stream(stream)))
+
+
+def osprey_kv8_attend(ctx: Ctx, kv: Kv8Cache, layer: int, n_rows: torch.Tensor, q: torch.Tensor, out: torch.Tensor,
+                      status: torch.Tensor, rotate: bool = False, advanced: bool = True, stream=None):
+    """Attention of each sequence's newest n_rows[b] rows; q [B, max_rows, Hq, hd] bf16 or float32 (rows may be views
+    into a wider projection's output), out dense and of q's type."""
+    s = ctx.shape
+    B = kv.page_table.shape[0]
+    if q.dim() != 4:
+        raise ValueError("q is [B, max_rows, Hq, hd]")
+    R = q.shape[1]
+    stride = _strided_rows(q, (B, R), (s.n_q_heads, s.head_dim), "q")
+    _need(n_rows, torch.int32, (B,), "n_rows")
+    _need(out, q.dtype, (B, R, s.n_q_heads, s.head_dim), "out")
+    _need(status, torch.int32, (1,), "status")
+    kvs = kv.c_struct(s)
+    _check(_c_kv8_attend(ctx.handle, ctypes.byref(kvs), layer, B, R, _ptr(n_rows), _ptr(q), _ROWS[q.dtype], stride,
+                         int(rotate), int(advanced), _ptr(out), _ptr(status), _stream(stream)))
 
 
 def osprey_draft_step(ctx: Ctx, kv: KvCache, n_new: torch.Tensor, tokens: torch.Tensor, feats: torch.Tensor,

@@ -8,6 +8,7 @@
 #include <cstring>
 #include <new>
 
+#include "attn8.cuh"
 #include "common.cuh"
 #include "draft.cuh"
 #include "tc.cuh"
@@ -367,6 +368,162 @@ extern "C" int osprey_kv_append(const osprey_ctx *ctx, const osprey_kv *kv, int 
     a.status = dev_status;
     cudaError_t e = launch_kv_append(a, (cudaStream_t)stream);
     return e == cudaSuccess ? OSPREY_OK : cuda_fail(e, "kv_append launch");
+}
+
+// ------------------------------------------------------------------ appending with the rotation, the 8-bit cache
+// A rotary frequency as a 64-bit fraction of a turn for each position.
+static void rope_freqs(const osprey_ctx *ctx, uint64_t (&freq)[64]) {
+    for (int i = 0; i < ctx->dim.hd / 2; ++i)
+        freq[i] = (uint64_t)std::ldexp(ctx->inv_freq[i] * 0.15915494309189535, 64);
+}
+
+// What both appending calls check and pass on.
+static int kv_rope_args(const osprey_ctx *ctx, int layer, int B, const int32_t *n_rows, int64_t total_rows,
+                        const void *k_rows, const void *v_rows, int rows_dtype, int64_t row_stride,
+                        int32_t *page_table, int32_t *seq_len, int max_pages, int n_pages, int32_t *status, KvRopeArgs &a) {
+    const Dims &D = ctx->dim;
+    if (B < 0 || B > 4096) return fail(OSPREY_ERR_INVALID_ARG, "B must be in 0..4096");
+    if (layer < -1 || layer >= D.L) return fail(OSPREY_ERR_INVALID_ARG, "layer must be -1 (all) or in 0..%d", D.L - 1);
+    if (total_rows < 0 || total_rows > (1LL << 40)) return fail(OSPREY_ERR_INVALID_ARG, "total_rows must be in 0..2^40");
+    if (rows_dtype != OSPREY_F32 && rows_dtype != OSPREY_BF16) return fail(OSPREY_ERR_DTYPE, "unknown rows dtype %d", rows_dtype);
+    if (!n_rows || !page_table || !seq_len) return fail(OSPREY_ERR_INVALID_ARG, "null pointer");
+    if (total_rows > 0 && (!k_rows || !v_rows)) return fail(OSPREY_ERR_INVALID_ARG, "null rows");
+    if (max_pages < 1 || max_pages >= (1 << 26) || n_pages < 1)
+        return fail(OSPREY_ERR_INVALID_ARG, "max_pages_per_seq in 1..2^26 - 1 and n_pages >= 1 required");
+    const int64_t dense = (int64_t)D.Hkv * D.hd;
+    if (row_stride == 0) row_stride = dense;
+    if (row_stride < dense || row_stride > (1LL << 24) || row_stride * (rows_dtype == OSPREY_F32 ? 4 : 2) % 16 ||
+        ((uintptr_t)k_rows | (uintptr_t)v_rows) % 16)
+        return fail(OSPREY_ERR_INVALID_ARG, "rows must start on 16 bytes, row_stride at least n_kv_heads * head_dim");
+    a.k_rows = k_rows;
+    a.v_rows = v_rows;
+    a.rows_f32 = rows_dtype == OSPREY_F32;
+    a.rotate = 1;
+    a.total_rows = total_rows;
+    a.row_stride = row_stride;
+    a.n_rows = n_rows;
+    a.page_table = page_table;
+    a.seq_len = seq_len;
+    a.B = B;
+    a.layers = layer < 0 ? D.L : 1;
+    a.layer0 = layer < 0 ? 0 : layer;
+    a.Hkv = D.Hkv;
+    a.hd = D.hd;
+    a.max_pages = max_pages;
+    a.n_pages = n_pages;
+    a.status = status;
+    rope_freqs(ctx, a.freq);
+    return OSPREY_OK;
+}
+
+extern "C" int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv, int layer, int B, const int32_t *n_rows,
+                                     int64_t total_rows, const void *k_rows, const void *v_rows, int rows_dtype,
+                                     int64_t row_stride, int advance, int32_t *dev_status, void *stream) {
+    g_err[0] = 0;
+    if (!ctx || !kv) return fail(OSPREY_ERR_INVALID_ARG, "null context or kv");
+    if (B == 0) return OSPREY_OK;
+    KvRopeArgs a{};
+    const int rc = kv_rope_args(ctx, layer, B, n_rows, total_rows, k_rows, v_rows, rows_dtype, row_stride,
+                                kv->page_table, kv->seq_len, kv->max_pages_per_seq, kv->n_pages, dev_status, a);
+    if (rc != OSPREY_OK) return rc;
+    if (!kv->k_pages || !kv->v_pages || ((uintptr_t)kv->k_pages | (uintptr_t)kv->v_pages) % 16)
+        return fail(OSPREY_ERR_INVALID_ARG, "K/V pages must be given and 16-byte aligned");
+    a.k_pages = (uint16_t *)kv->k_pages;
+    a.v_pages = (uint16_t *)kv->v_pages;
+    const cudaError_t e = launch_kv_rope(a, false, advance != 0, (cudaStream_t)stream);
+    return e == cudaSuccess ? OSPREY_OK : cuda_fail(e, "kv_append_rope launch");
+}
+
+static int kv8_check(const osprey_kv8 *kv) {
+    if (!kv->k8 || !kv->v8 || !kv->k_scale || !kv->v_scale || !kv->k_tail || !kv->v_tail || !kv->page_table || !kv->seq_len)
+        return fail(OSPREY_ERR_INVALID_ARG, "null pointer in the 8-bit cache");
+    if (((uintptr_t)kv->k8 | (uintptr_t)kv->v8 | (uintptr_t)kv->k_tail | (uintptr_t)kv->v_tail) % 16 ||
+        ((uintptr_t)kv->k_scale | (uintptr_t)kv->v_scale) % 4)
+        return fail(OSPREY_ERR_INVALID_ARG, "codes and tails must be 16-byte aligned, scales 4-byte");
+    if (kv->max_pages_per_seq < 1 || kv->max_pages_per_seq >= (1 << 26) || kv->n_pages < 1 || kv->tail_pages < 1)
+        return fail(OSPREY_ERR_INVALID_ARG, "max_pages_per_seq in 1..2^26 - 1, n_pages >= 1 and tail_pages >= 1 required");
+    return OSPREY_OK;
+}
+
+extern "C" int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, int B, const int32_t *n_rows,
+                                 int64_t total_rows, const void *k_rows, const void *v_rows, int rows_dtype,
+                                 int64_t row_stride, int rotate, int advance, int32_t *dev_status, void *stream) {
+    g_err[0] = 0;
+    if (!ctx || !kv) return fail(OSPREY_ERR_INVALID_ARG, "null context or kv");
+    if (B == 0) return OSPREY_OK;
+    KvRopeArgs a{};
+    int rc = kv8_check(kv);
+    if (rc == OSPREY_OK)
+        rc = kv_rope_args(ctx, layer, B, n_rows, total_rows, k_rows, v_rows, rows_dtype, row_stride,
+                          kv->page_table, kv->seq_len, kv->max_pages_per_seq, kv->n_pages, dev_status, a);
+    if (rc != OSPREY_OK) return rc;
+    a.rotate = rotate != 0;
+    a.k8 = (uint8_t *)kv->k8;
+    a.v8 = (uint8_t *)kv->v8;
+    a.k_scale = kv->k_scale;
+    a.v_scale = kv->v_scale;
+    a.k_tail = (uint16_t *)kv->k_tail;
+    a.v_tail = (uint16_t *)kv->v_tail;
+    a.tail_pages = kv->tail_pages;
+    const cudaError_t e = launch_kv_rope(a, true, advance != 0, (cudaStream_t)stream);
+    return e == cudaSuccess ? OSPREY_OK : cuda_fail(e, "kv8_append launch");
+}
+
+// One layer's part of the 8-bit cache, as attention reads it.
+static void attn8_layer(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, int B, Attn8Args &a) {
+    const Dims &D = ctx->dim;
+    const size_t blk = (size_t)layer * kv->n_pages * D.Hkv, page = (size_t)16 * D.hd;
+    const size_t tail = (size_t)layer * B * kv->tail_pages * D.Hkv * page;
+    a.B = B;
+    a.Hq = D.Hq;
+    a.Hkv = D.Hkv;
+    a.hd = D.hd;
+    a.k8 = (const uint8_t *)kv->k8 + blk * page;
+    a.v8 = (const uint8_t *)kv->v8 + blk * page;
+    a.k_scale = kv->k_scale + blk;
+    a.v_scale = kv->v_scale + blk;
+    a.k_tail = (const uint16_t *)kv->k_tail + tail;
+    a.v_tail = (const uint16_t *)kv->v_tail + tail;
+    a.page_table = kv->page_table;
+    a.max_pages = kv->max_pages_per_seq;
+    a.n_pages = kv->n_pages;
+    a.tail_pages = kv->tail_pages;
+}
+
+extern "C" int osprey_kv8_attend(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, int B, int max_rows,
+                                 const int32_t *n_rows, const void *q, int dtype, int64_t q_stride, int rotate,
+                                 int advanced, void *out, int32_t *dev_status, void *stream) {
+    g_err[0] = 0;
+    if (!ctx || !kv) return fail(OSPREY_ERR_INVALID_ARG, "null context or kv");
+    if (B == 0) return OSPREY_OK;
+    const Dims &D = ctx->dim;
+    if (B < 0 || B > 4096) return fail(OSPREY_ERR_INVALID_ARG, "B must be in 0..4096");
+    if (layer < 0 || layer >= D.L) return fail(OSPREY_ERR_INVALID_ARG, "layer must be in 0..%d", D.L - 1);
+    if (max_rows < 1 || max_rows > 64) return fail(OSPREY_ERR_INVALID_ARG, "max_rows must be in 1..64");
+    if (dtype != OSPREY_F32 && dtype != OSPREY_BF16) return fail(OSPREY_ERR_DTYPE, "unknown dtype %d", dtype);
+    const int rc = kv8_check(kv);
+    if (rc != OSPREY_OK) return rc;
+    if (!n_rows || !q || !out) return fail(OSPREY_ERR_INVALID_ARG, "null pointer");
+    const int64_t dense = (int64_t)D.Hq * D.hd;
+    if (q_stride == 0) q_stride = dense;
+    if (q_stride < dense || q_stride > (1LL << 24) || q_stride * (dtype == OSPREY_F32 ? 4 : 2) % 16 ||
+        ((uintptr_t)q | (uintptr_t)out) % 16)
+        return fail(OSPREY_ERR_INVALID_ARG, "q and out must start on 16 bytes, q_stride at least n_q_heads * head_dim");
+    Attn8Args a{};
+    attn8_layer(ctx, kv, layer, B, a);
+    a.max_rows = max_rows;
+    a.seq_len = kv->seq_len;
+    a.n_rows = n_rows;
+    a.advanced = advanced != 0;
+    a.q = q;
+    a.q_f32 = dtype == OSPREY_F32;
+    a.rotate = rotate != 0;
+    a.q_stride = q_stride;
+    rope_freqs(ctx, a.freq);
+    a.out = out;
+    a.status = dev_status;
+    const cudaError_t e = launch_attn8(a, ctx->sms, (cudaStream_t)stream);
+    return e == cudaSuccess ? OSPREY_OK : cuda_fail(e, "kv8_attend launch");
 }
 
 // ------------------------------------------------------------------ draft step

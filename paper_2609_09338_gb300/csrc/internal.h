@@ -134,5 +134,8 @@ struct KvAppendArgs {
     int32_t *status;
 };
 cudaError_t launch_kv_append(const KvAppendArgs &a, cudaStream_t s);
+// The checks and the committed lengths alone; behind: right behind this call's own
+// kernel that reads them (and triggers its dependents).
+cudaError_t launch_kv_advance(const KvAppendArgs &a, bool behind, cudaStream_t s);
 
 }  // namespace osp

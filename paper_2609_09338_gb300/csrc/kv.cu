@@ -165,13 +165,17 @@ cudaError_t launch_kv_append(const KvAppendArgs &a, cudaStream_t s) {
         e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
+    return launch_kv_advance(a, a.total_rows > 0, s);
+}
+
+cudaError_t launch_kv_advance(const KvAppendArgs &a, bool behind, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((a.B + KV_THREADS / 32 - 1) / (KV_THREADS / 32));
     cfg.blockDim = dim3(KV_THREADS);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = a.total_rows > 0;   // only behind this call's own scatter
+    attr[0].val.programmaticStreamSerializationAllowed = behind;   // only behind this call's own scatter
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_advance, a);

@@ -1,0 +1,100 @@
+// The 8-bit paged K/V cache and appending with the rotation: what its kernels share.
+//
+// A block is one page (16 positions) of one KV head.  Finished blocks hold e4m3
+// codes x / s with one scale s a block, a power of two: the smallest that brings the
+// block's largest magnitude to 448 or less (not below 2^-100).  e4m3 has the same
+// four significant bits at every magnitude, so a scale that is no power of two
+// would gain nothing but a rounding of its own.  A block with a value that is not
+// finite has the scale NaN and codes 0.
+//
+// The codes lie as the tensor cores read them, in core matrices of 8 rows x 16
+// bytes, so that a page goes to shared memory by plain bulk copies and is an
+// operand as it lands:
+//   K (the reduction runs over dims):   [slot / 8][dim / 16][slot % 8][dim % 16]
+//   V (the reduction runs over slots):  [dim][slot]
+// Rows of the unfinished page stay in bf16 in the tail, a ring of tail_pages pages
+// a sequence that always holds the last rows appended: each value is rounded to 8
+// bits once, with its block's final scale, however many calls append the block.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace osp {
+
+constexpr int KV8_MIN_EXP = -100;
+
+__device__ __forceinline__ uint64_t rope_fix(uint64_t freq, int pos) { return freq * (uint64_t)pos; }
+
+// cos and sin of pos * inv_freq.  freq is inv_freq / 2 pi as a 64-bit fraction of a
+// turn: the product modulo 2^64 drops whole turns exactly, which in double costs
+// five instructions of a pipe that is 1/64 as wide.
+__device__ __forceinline__ void rope_cs_fix(uint64_t freq, int pos, float &c, float &s) {
+    const int turn = (int)(rope_fix(freq, pos) >> 32);      // in 2^-32 turns, -1/2 .. 1/2
+    sincospif((float)turn * 0x1p-31f, &s, &c);
+}
+
+// bf16(x1) : bf16(x0), rounded to nearest even; NaN stays NaN
+__device__ __forceinline__ uint32_t kv8_bf2(float x0, float x1) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(x1), "f"(x0));
+    return r;
+}
+// e4m3(x1) : e4m3(x0), rounded to nearest even
+__device__ __forceinline__ uint32_t e4m3x2(float x0, float x1) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(x1), "f"(x0));
+    return r;
+}
+// the two values of a pair of codes
+__device__ __forceinline__ float2 e4m3x2_f(uint32_t pair) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)pair));
+    float lo, hi;
+    asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.f32.f16 %0, a;\ncvt.f32.f16 %1, b;\n}" : "=f"(lo), "=f"(hi) : "r"(h));
+    return make_float2(lo, hi);
+}
+
+// The largest bf16 magnitude of a block as its scale's exponent: smallest k >= -100
+// with a <= 448 * 2^k = 1.75 * 2^(k + 8).
+__device__ __forceinline__ int kv8_exp(uint32_t mag) {
+    const int e = (int)(mag >> 7) - 127 - 8 + ((mag & 0x7f) > 0x60 ? 1 : 0);
+    return e < KV8_MIN_EXP ? KV8_MIN_EXP : e;
+}
+__device__ __forceinline__ float kv8_pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+
+struct KvRopeArgs {
+    const void *k_rows, *v_rows;   // [layers][total_rows] rows row_stride elements apart, each [Hkv][hd]
+    int rows_f32, rotate;
+    int64_t total_rows, row_stride;
+    const int32_t *n_rows;         // [B]
+    const int32_t *page_table;
+    int32_t *seq_len;
+    int B, layers, layer0, Hkv, hd, max_pages, n_pages;
+    int32_t *status;
+    uint64_t freq[64];
+    // bf16 cache
+    uint16_t *k_pages, *v_pages;
+    // 8-bit cache
+    uint8_t *k8, *v8;
+    float *k_scale, *v_scale;
+    uint16_t *k_tail, *v_tail;
+    int tail_pages;
+};
+cudaError_t launch_kv_rope(const KvRopeArgs &a, bool eight, bool advance, cudaStream_t s);
+
+// Quantises the pages that positions pos0[b] .. pos0[b] + nnew[b] - 1 of valid
+// sequences finish, from the tail (every layer).
+struct Kv8PackArgs {
+    int B, L, Hkv, hd, max_pages, n_pages, tail_pages, max_new;
+    const int *valid, *pos0, *nnew;
+    const int32_t *page_table;
+    uint8_t *k8, *v8;
+    float *k_scale, *v_scale;
+    const uint16_t *k_tail, *v_tail;
+};
+cudaError_t launch_kv8_pack(const Kv8PackArgs &a, cudaStream_t s);
+
+}  // namespace osp

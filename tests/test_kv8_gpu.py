@@ -1,0 +1,462 @@
+"""The 8-bit cache: codes, scales and tail bit for bit against the oracle, whatever calls appended them; attention over
+it against float64."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import kv8 as o8  # noqa: E402
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    import __graft_entry__ as g
+    g.build()
+
+
+def _cache(ctx, B, max_pages, seed, tail=2):
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    tab, n = kc.table(B, max_pages, seed)
+    kv = ob.alloc_kv8(ctx.shape, tab, n, tail)
+    # what is never written may be anything
+    kv.k8.fill_(0x7f)
+    kv.v8.fill_(0x7f)
+    kv.k_scale.fill_(float("nan"))
+    kv.v_scale.fill_(float("nan"))
+    kv.k_tail.fill_(float("nan"))
+    kv.v_tail.fill_(float("nan"))
+    return kv, torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def _ints(n):
+    return torch.tensor(n, dtype=torch.int32, device="cuda")
+
+
+def _dbl(t):
+    return t.double().cpu().numpy()
+
+
+# ---------------------------------------------------------------- appending
+@pytest.mark.parametrize("Hkv,hd,L", [(2, 64, 1), (8, 128, 1), (1, 128, 2), (3, 64, 2)])
+@pytest.mark.parametrize("tail", [1, 2, 3])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_codes_scales_and_tail(Hkv, hd, L, tail, dtype):
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(4 * Hkv, Hkv, hd, L)
+    gen = torch.Generator(device="cuda").manual_seed(hd + Hkv)
+    counts = [[0, 1, 15, 16, 17, 70], [1, 1, 1, 1, 1, 1], [40, 15, 0, 33, 14, 9], [1, 16, 16, 1, 50, 2]]
+    B = len(counts[0])
+    kv, st = _cache(ctx, B, 10, 3, tail)
+    model, at = kc.Model(L, B), np.zeros(B, int)
+    for i, n in enumerate(counts):
+        k, v = (kc.rows(gen, (L, sum(n), Hkv, hd), dtype, 3 * Hkv * hd if i % 2 else None) for _ in range(2))
+        k.mul_(torch.exp2(torch.randint(-6, 7, (hd,), generator=gen, device="cuda")).to(dtype))
+        ob.osprey_kv8_append(ctx, kv, _ints(n), k, v, st, rotate=False)
+        torch.cuda.synchronize()
+        at += np.array(n)
+        assert int(st.item()) == 0 and kv.seq_len.tolist() == at.tolist()
+        model.append(n, _dbl(k.to(BF)), _dbl(v.to(BF)))
+        model.check(kv, at)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_rotated_rows_are_those_of_the_bf16_cache(hd):
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 4, hd)
+    gen = torch.Generator(device="cuda").manual_seed(hd)
+    kv, st = _cache(ctx, 3, 8, 3)
+    tab, n = kc.table(3, 8, 5)
+    bf = ob.alloc_kv(ctx.shape, tab, n)
+    model, at = kc.Model(1, 3), np.zeros(3, int)
+    for n in ([17, 3, 64], [1, 15, 40]):
+        k, v = (kc.rows(gen, (1, sum(n), 4, hd), F32) for _ in range(2))
+        ob.osprey_kv8_append(ctx, kv, _ints(n), k, v, st)
+        ob.osprey_kv_append_rope(ctx, bf, _ints(n), k, v, st)
+        torch.cuda.synchronize()
+        ks, vs = _dbl(bf.k_pages), _dbl(bf.v_pages)
+        got = []
+        for x in (ks, vs):
+            got.append(np.concatenate([x[:, tab[b][t // 16], :, t % 16].transpose(1, 0, 2, 3) if False else
+                                       np.moveaxis(x[:, tab[b][t // 16], :, t % 16], 0, 1)
+                                       for b in range(3) for t in [np.arange(at[b], at[b] + n[b])]], 1))
+        model.append(n, *got)
+        at += np.array(n)
+        model.check(kv, at)
+    assert int(st.item()) == 0
+
+
+def test_one_layer_without_advancing_and_rows_taken_back():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 4, 64, 2)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    kv, st = _cache(ctx, 2, 8, 3, tail=3)
+    model = kc.Model(2, 2)
+    n = [20, 31]
+    k, v = (kc.rows(gen, (2, 51, 4, 64), BF) for _ in range(2))
+    for l in range(2):
+        ob.osprey_kv8_append(ctx, kv, _ints(n), k[l], v[l], st, layer=l, rotate=False, advance=l == 1)
+    model.append(n, _dbl(k), _dbl(v))
+    torch.cuda.synchronize()
+    model.check(kv, n)
+    # sequence 0 takes 6 rows back (its second page is unfinished again), sequence 1 takes 17
+    kv.seq_len.copy_(_ints([14, 14]))
+    for l in range(2):
+        for b in range(2):
+            model.k[l][b], model.v[l][b] = model.k[l][b][:14], model.v[l][b][:14]
+    k, v = (kc.rows(gen, (2, 30, 4, 64), BF) for _ in range(2))
+    ob.osprey_kv8_append(ctx, kv, _ints([1, 29]), k, v, st, rotate=False)
+    model.append([1, 29], _dbl(k), _dbl(v))
+    torch.cuda.synchronize()
+    model.check(kv, [15, 43])
+    assert int(st.item()) == 0 and kv.seq_len.tolist() == [15, 43]
+
+
+def test_extreme_blocks():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(4, 2, 128)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    kv, st = _cache(ctx, 1, 8, 3)
+    n = 7 * 16
+    k, v = (kc.rows(gen, (1, n, 2, 128), BF) for _ in range(2))
+    k[0, 0:16] = 0
+    v[0, 0:16] *= 2.0 ** -125
+    k[0, 16:32] *= 2.0 ** 120
+    k[0, 20, 1, 7], v[0, 33, 0, 99], k[0, 49, 1, 127], v[0, 64, 1, 0] = float("inf"), float("nan"), -float("inf"), float("inf")
+    k[0, 80, 0, :] = torch.tensor([448.0, -450.0] * 64)
+    k[0, 96:, 0, 0] = 448.0
+    k[0, 96:, 0, 1:] = torch.randn((16, 127), generator=gen, device="cuda").to(BF)
+    ob.osprey_kv8_append(ctx, kv, _ints([n]), k, v, st, rotate=False)
+    torch.cuda.synchronize()
+    model = kc.Model(1, 1)
+    model.append([n], _dbl(k), _dbl(v))
+    model.check(kv, [n])
+
+
+@pytest.mark.parametrize("advance", [True, False])
+def test_append_errors_leave_the_sequence(advance):
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(4, 2, 64)
+    for n, bad in (([20, 20, 20], "page"), ([20, 20, 65], "table")):
+        kv, st = _cache(ctx, 3, 4, 2)
+        left = 1 if bad == "page" else 2
+        if bad == "page":
+            kv.page_table[1, 1] = -1
+        k = torch.ones((1, sum(n), 2, 64), dtype=BF, device="cuda")
+        ob.osprey_kv8_append(ctx, kv, _ints(n), k, k, st, advance=advance)
+        torch.cuda.synchronize()
+        assert int(st.item()) == -4
+        assert kv.seq_len.tolist() == [20 if advance and b != left else 0 for b in range(3)]
+        ring = kv.k_tail[0, 2 * left:2 * left + 2].float()
+        assert torch.isnan(ring).all() and not torch.isnan(kv.k_tail[0, 0].float()).any()
+        tab = kv.page_table.cpu().numpy()
+        assert (kv.k8[0, [p for p in tab[left] if p >= 0]] == 0x7f).all()
+    for n in ([3, 4], [9, -1]):
+        kv, st = _cache(ctx, 2, 4, 2)
+        k = torch.ones((1, 8, 2, 64), dtype=BF, device="cuda")
+        ob.osprey_kv8_append(ctx, kv, _ints(n), k, k, st, advance=advance)
+        torch.cuda.synchronize()
+        assert int(st.item()) == -1 and kv.seq_len.tolist() == [0, 0] and torch.isnan(kv.k_tail.float()).all()
+
+
+# ---------------------------------------------------------------- attention
+def _fill(ctx, kv, st, lens, gen, spread=1.0):
+    """A cache of lens rows a sequence; the float64 values that attention sees, for layer 0 [T, Hkv, hd] a sequence."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    s = ctx.shape
+    k, v = (kc.rows(gen, (s.n_layers, sum(lens), s.n_kv_heads, s.head_dim), BF) for _ in range(2))
+    k.mul_(spread)
+    ob.osprey_kv8_append(ctx, kv, _ints(lens), k, v, st, rotate=False)
+    return k, v
+
+
+def _seen(x, lens):
+    """[T, Hkv, hd] float64 of each sequence, finished pages through 8 bits (the oracle's rounding, vectorised)."""
+    out, r = [], 0
+    tab = o8.e4m3_values()
+    for n in lens:
+        y = _dbl(x[r:r + n]).copy()
+        r += n
+        f = n // 16 * 16
+        if f:
+            blk = y[:f].reshape(f // 16, 16, *y.shape[1:])
+            a = np.abs(blk).max((1, 3), keepdims=True)
+            e = np.maximum(-100.0, np.ceil(np.log2(np.maximum(a, 1e-300) / 448.0)))
+            e = np.where(a > 448 * 2.0 ** e, e + 1, e)
+            z = np.abs(blk) / 2.0 ** e
+            hi = np.clip(np.searchsorted(tab, z), 1, 126)
+            up, dn = tab[hi] - z, z - tab[hi - 1]
+            q = np.where((up < dn) | ((up == dn) & (hi % 2 == 0)), hi, hi - 1)
+            y[:f] = (np.sign(blk) * tab[q] * 2.0 ** e).reshape(f, *y.shape[1:])
+        out.append(y)
+    return out
+
+
+def _check(q, out, n, lens, ks, vs, dtype, sentinel):
+    """Each output against float64.  Weights: the score's float32 sum (2^-17 of max |q| sum |k| / sqrt(hd), natural
+    units), 2^-20 of the exponential and, in bf16 calls, 2^-11 of the planes; an error d in every weight moves an
+    output by at most 2 d max |V|.  Then the rounding to the output's type."""
+    G = q.shape[2] // ks[0].shape[1]
+    qd, od = _dbl(q), _dbl(out)
+    for b, (m, T) in enumerate(zip(n, lens)):
+        assert (od[b, m:] == sentinel).all()
+        if not m:
+            continue
+        want = o8.attend(qd[b, :m], ks[b][:T], vs[b][:T])
+        H = ks[b].shape[1]
+        for h in range(H):
+            qq = np.abs(qd[b, :m, h * G:(h + 1) * G]).max()
+            a = qq * np.abs(ks[b][:T, h]).sum(1).max() / np.sqrt(q.shape[3])
+            top = np.abs(vs[b][:T, h]).max(0)
+            d = 2.0 ** -17 * a + 2.0 ** -20 + (2.0 ** -11 if dtype is BF else 0.0)
+            w = want[:, h * G:(h + 1) * G]
+            tol = 2 * d * top + (2.0 ** -8 if dtype is BF else 2.0 ** -23) * np.abs(w)
+            err = np.abs(od[b, :m, h * G:(h + 1) * G] - w)
+            assert (err <= tol).all(), (b, h, float((err / tol).max()))
+
+
+CASES = [(4, 2, 64), (16, 8, 128), (4, 4, 128), (16, 4, 128), (8, 1, 64), (16, 2, 128)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,hd", CASES)
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("advanced", [True, False])
+def test_single_rows(Hq, Hkv, hd, dtype, advanced):
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(Hq, Hkv, hd)
+    gen = torch.Generator(device="cuda").manual_seed(Hq + hd)
+    lens = [1, 2, 15, 16, 17, 31, 32, 33, 47, 127, 128, 129, 144, 255, 256, 272, 700, 0, 2001]
+    kv, st = _cache(ctx, len(lens), 128, 5)
+    k, v = _fill(ctx, kv, st, lens, gen)
+    n = [0 if t in (0, 47) else 1 for t in lens]
+    if not advanced:
+        kv.seq_len.sub_(_ints(n))
+    q = kc.rows(gen, (len(lens), 1, Hq, hd), dtype)
+    out = torch.full_like(q, 9.0)
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints(n), q, out, st, advanced=advanced)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    _check(q, out, n, lens, _seen(k[0], lens), _seen(v[0], lens), dtype, 9.0)
+
+
+@pytest.mark.parametrize("Hq,Hkv,hd", CASES)
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [2, 5, 17, 64])
+def test_many_rows(Hq, Hkv, hd, dtype, rows):
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(Hq, Hkv, hd)
+    gen = torch.Generator(device="cuda").manual_seed(Hq + hd + rows)
+    rng = np.random.default_rng(rows)
+    n = [rows, 1, max(1, rows - 1), 0, int(rng.integers(1, rows + 1)), rows]
+    lens = [rows, 40, 130 + rows, 64, 300, 1025]
+    kv, st = _cache(ctx, len(lens), 70, 5)
+    k, v = _fill(ctx, kv, st, lens, gen)
+    q = kc.rows(gen, (len(lens), rows, Hq, hd), dtype, width=(Hq + 2 * Hkv) * hd)
+    out = torch.full((len(lens), rows, Hq, hd), 9.0, dtype=dtype, device="cuda")
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints(n), q, out, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    _check(q, out, n, lens, _seen(k[0], lens), _seen(v[0], lens), dtype, 9.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_peaked_scores(dtype):
+    """Scores of tens to hundreds: the maximum moves from key to key, and small weights vanish."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(16, 4, 128)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lens = [900, 130, 2048]
+    kv, st = _cache(ctx, 3, 128, 5)
+    k, v = _fill(ctx, kv, st, lens, gen, spread=8.0)
+    q = kc.rows(gen, (3, 3, 16, 128), dtype) * 2
+    out = torch.zeros_like(q)
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints([3, 3, 3]), q, out, st)
+    torch.cuda.synchronize()
+    _check(q, out, [3, 3, 3], lens, _seen(k[0], lens), _seen(v[0], lens), dtype, 0.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rotated_queries(dtype):
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 2, 128)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lens, n = [300, 40, 17], [4, 1, 3]
+    kv, st = _cache(ctx, 3, 32, 5)
+    k, v = _fill(ctx, kv, st, lens, gen)
+    q = kc.rows(gen, (3, 4, 8, 128), dtype)
+    got, want = torch.zeros((3, 4, 8, 128), dtype=F32, device="cuda"), torch.zeros((3, 4, 8, 128), dtype=F32, device="cuda")
+    turned = np.zeros(q.shape)
+    for b in range(3):
+        turned[b, :n[b]] = o8.rotate_rows(_dbl(q[b, :n[b]]), lens[b] - n[b], kc.THETA)
+    out = torch.zeros_like(q)
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints(n), q, out, st, rotate=True)
+    torch.cuda.synchronize()
+    # a turned query keeps more bits than its type has: it enters as it is, in float32 or as two planes (8 bits)
+    ref = torch.from_numpy(turned)
+    extra = 2.0 ** -8 if dtype is BF else 2.0 ** -20
+    ks, vs = _seen(k[0], lens), _seen(v[0], lens)
+    for b in range(3):
+        w = o8.attend(turned[b, :n[b]], ks[b], vs[b])
+        a = np.abs(turned[b, :n[b]]).max() * np.abs(ks[b]).sum(2).max() / np.sqrt(128)
+        top = np.abs(vs[b]).max()
+        g = _dbl(out[b, :n[b]])
+        # 2^-8 of each term of the score, of random sign over 128 terms (6 of their standard deviations)
+        d = extra * 6 * np.linalg.norm(np.abs(turned[b, :n[b]]).max() * np.abs(ks[b]).max((0, 1))) / np.sqrt(128) + 2.0 ** -17 * a
+        assert (np.abs(g - w) <= 2 * d * top + 2.0 ** -8 * np.abs(w) + 2.0 ** -10 * top).all()
+    del got, want, ref
+
+
+def test_values_behind_a_row_do_not_reach_it():
+    """NaN and infinities in later rows of the tail and in finished pages that a row does not see."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 4, 128)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lens = [70, 75]
+    (kv, st), (clean, _) = _cache(ctx, 2, 8, 5), _cache(ctx, 2, 8, 5)
+    k, v = (kc.rows(gen, (1, 145, 4, 128), BF) for _ in range(2))
+    ob.osprey_kv8_append(ctx, clean, _ints(lens), k, v, st, rotate=False)
+    k, v = k.clone(), v.clone()
+    k[0, 66], v[0, 67] = float("nan"), float("inf")      # sequence 0: rows 66 and 67, in the tail
+    v[0, 70 + 50, 1, 3] = float("nan")                    # sequence 1: row 50, in its fourth page
+    ob.osprey_kv8_append(ctx, kv, _ints(lens), k, v, st, rotate=False)
+    q = kc.rows(gen, (2, 40, 8, 128), BF)
+    outs = []
+    for c in (kv, clean):
+        o = torch.zeros_like(q)
+        ob.osprey_kv8_attend(ctx, c, 0, _ints([40, 40]), q, o, st)
+        outs.append(o)
+    torch.cuda.synchronize()
+    got, want = outs
+    assert torch.equal(got[0, :36], want[0, :36])                        # positions 30 .. 65
+    assert torch.isnan(got[0, 36:37]).all() and not torch.isfinite(got[0, 37:]).any()
+    assert torch.equal(got[1, :13], want[1, :13])                        # 35 .. 47 see pages 0 to 2
+    assert torch.isnan(got[1, 13:, 2:4]).all() and torch.equal(got[1, 13:, 4:], want[1, 13:, 4:])
+
+
+def test_non_finite_queries_stay_in_their_row():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 2, 64)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    kv, st = _cache(ctx, 1, 16, 5)
+    _fill(ctx, kv, st, [200], gen)
+    q = kc.rows(gen, (1, 3, 8, 64), F32)
+    want, got = torch.zeros_like(q), torch.zeros_like(q)
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints([3]), q, want, st)
+    q[0, 1, 2, 5], q[0, 2, 7, 0] = float("nan"), float("inf")
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints([3]), q, got, st)
+    torch.cuda.synchronize()
+    bad = torch.zeros((3, 8), dtype=torch.bool, device="cuda")
+    bad[1, 2] = bad[2, 7] = True
+    assert torch.isnan(got[0][bad]).all() and torch.equal(got[0][~bad], want[0][~bad])
+
+
+def test_attend_errors_zero_the_sequence():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 2, 64)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for what, code in (("page", -4), ("rows", -1), ("more rows than keys", -1), ("length", -4), ("negative", -1)):
+        kv, st = _cache(ctx, 3, 16, 5)
+        lens, n = [200, 180, 250], [2, 2, 2]
+        _fill(ctx, kv, st, lens, gen)
+        if what == "page":
+            kv.page_table[1, 7] = kv.n_pages
+        elif what == "rows":
+            n[1] = 3
+        elif what == "more rows than keys":
+            kv.seq_len[1] = 1
+        elif what == "length":
+            kv.seq_len[1] = 16 * 16 + 1
+        else:
+            kv.seq_len[1] = -5
+        q = kc.rows(gen, (3, 2, 8, 64), BF)
+        out = torch.full_like(q, 9.0)
+        ob.osprey_kv8_attend(ctx, kv, 0, _ints(n), q, out, st)
+        torch.cuda.synchronize()
+        assert int(st.item()) == code, what
+        assert not out[1].any() and (out[0] != 9).any() and out[0].any() and out[2].any(), what
+
+
+def test_second_layer_and_another_stream():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 4, 64, 3)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lens = [77, 300]
+    kv, st = _cache(ctx, 2, 24, 5)
+    k, v = _fill(ctx, kv, st, lens, gen)
+    q = kc.rows(gen, (2, 2, 8, 64), BF)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for l in range(3):
+        out = torch.zeros_like(q)
+        side.wait_stream(torch.cuda.current_stream())
+        ob.osprey_kv8_attend(ctx, kv, l, _ints([2, 2]), q, out, st, stream=side)
+        torch.cuda.synchronize()
+        _check(q, out, [2, 2], lens, _seen(k[l], lens), _seen(v[l], lens), BF, 0.0)
+
+
+# ---------------------------------------------------------------- together
+@pytest.mark.parametrize("graph", [False, True])
+def test_decoding_with_the_cache(graph):
+    """A prompt, then token after token: append with the rotation, attend with rotated queries; eager or replayed."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 2, 128)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    B, hd, H = 3, 128, 2
+    kv, st = _cache(ctx, B, 8, 5)
+    lens = np.array([30, 1, 63])
+    k, v = (kc.rows(gen, (1, int(lens.sum()), H, hd), BF) for _ in range(2))
+    ob.osprey_kv8_append(ctx, kv, _ints(lens.tolist()), k, v, st)
+    raw_k = [list(x) for x in np.split(_dbl(k[0]), np.cumsum(lens)[:-1])]
+    raw_v = [list(x) for x in np.split(_dbl(v[0]), np.cumsum(lens)[:-1])]
+    one = _ints([1] * B)
+    qkv = torch.zeros((B, 1, (8 + 2 * H) * hd), dtype=BF, device="cuda")
+    q = qkv[..., :8 * hd].unflatten(-1, (8, hd))
+    kn = qkv[:, 0, 8 * hd:(8 + H) * hd].unflatten(-1, (H, hd))
+    vn = qkv[:, 0, (8 + H) * hd:].unflatten(-1, (H, hd))
+    out = torch.zeros((B, 1, 8, hd), dtype=BF, device="cuda")
+
+    def step():
+        ob.osprey_kv8_append(ctx, kv, one, kn, vn, st, layer=0)
+        ob.osprey_kv8_attend(ctx, kv, 0, one, q, out, st, rotate=True)
+
+    if graph:
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            step()
+    for i in range(36):
+        qkv.copy_(torch.randn(qkv.shape, generator=gen, device="cuda"))
+        g.replay() if graph else step()
+        torch.cuda.synchronize()
+        lens = lens + 1
+        for b in range(B):
+            raw_k[b].append(_dbl(kn[b]))
+            raw_v[b].append(_dbl(vn[b]))
+            if i % 7:
+                continue
+            T = len(raw_k[b])
+            turned = torch.from_numpy(o8.rotate_rows(np.array(raw_k[b]), 0, kc.THETA)).to(BF)
+            ks = _seen(turned, [T])[0]
+            vs = _seen(torch.from_numpy(np.array(raw_v[b])).to(BF), [T])[0]
+            want = o8.attend(o8.rotate_rows(_dbl(q[b]), T - 1, kc.THETA), ks, vs)
+            # a key that rounds to the other bf16 or e4m3 neighbour, a query of 8 bits: percents of a weight
+            assert np.abs(_dbl(out[b]) - want).max() <= 0.05 * np.abs(vs).max()
+    assert int(st.item()) == 0 and kv.seq_len.tolist() == lens.tolist()
