@@ -259,6 +259,9 @@ class Kv8Cache:
     page_table: torch.Tensor   # [B, max_pages] int32
     seq_len: torch.Tensor      # [B] int32
 
+    def __post_init__(self):
+        self._key = self._struct = None
+
     @property
     def max_pages(self) -> int:
         return self.page_table.shape[1]
@@ -269,23 +272,33 @@ class Kv8Cache:
 
     @property
     def tail_pages(self) -> int:
-        return self.k_tail.shape[1] // self.page_table.shape[0]
+        return self.k_tail.shape[1] // max(1, self.page_table.shape[0])
 
     def c_struct(self, shape: DrafterShape) -> osprey_kv8:
-        """The C struct, after the checks of the tensors against the drafter's shape."""
+        """The C struct, after the checks of the tensors against the drafter's shape (made again when a tensor's
+        memory or size is not what it was at the last call)."""
+        k8, v8, ks, vs, kt, vt = self.k8, self.v8, self.k_scale, self.v_scale, self.k_tail, self.v_tail
+        tab, n = self.page_table, self.seq_len
+        key = (shape, k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), kt.data_ptr(), vt.data_ptr(),
+               tab.data_ptr(), n.data_ptr(), k8.numel(), v8.numel(), ks.numel(), vs.numel(), kt.numel(), vt.numel(),
+               tab.shape, n.numel())
+        if key == self._key:
+            return self._struct
         L, H, hd = shape.n_layers, shape.n_kv_heads, shape.head_dim
-        B, n, t = self.page_table.shape[0], self.n_pages, self.tail_pages
-        _need(self.k8, torch.uint8, (L, n, H, 16 * hd), "k8")
-        _need(self.v8, torch.uint8, (L, n, H, 16 * hd), "v8")
-        _need(self.k_scale, torch.float32, (L, n, H), "k_scale")
-        _need(self.v_scale, torch.float32, (L, n, H), "v_scale")
-        _need(self.k_tail, torch.bfloat16, (L, B * t, H, 16, hd), "k_tail")
-        _need(self.v_tail, torch.bfloat16, (L, B * t, H, 16, hd), "v_tail")
-        _need(self.page_table, torch.int32, None, "page_table")
-        _need(self.seq_len, torch.int32, (B,), "seq_len")
-        return osprey_kv8(self.k8.data_ptr(), self.v8.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
-                          self.k_tail.data_ptr(), self.v_tail.data_ptr(), self.page_table.data_ptr(),
-                          self.seq_len.data_ptr(), self.max_pages, n, t)
+        _need(tab, torch.int32, None, "page_table")
+        if tab.dim() != 2 or k8.dim() != 4:
+            raise ValueError("page_table is [B, max_pages], k8 [L, n_pages, Hkv, 16 * hd]")
+        B, pages, t = tab.shape[0], self.n_pages, self.tail_pages
+        _need(k8, torch.uint8, (L, pages, H, 16 * hd), "k8")
+        _need(v8, torch.uint8, (L, pages, H, 16 * hd), "v8")
+        _need(ks, torch.float32, (L, pages, H), "k_scale")
+        _need(vs, torch.float32, (L, pages, H), "v_scale")
+        _need(kt, torch.bfloat16, (L, B * t, H, 16, hd), "k_tail")
+        _need(vt, torch.bfloat16, (L, B * t, H, 16, hd), "v_tail")
+        _need(n, torch.int32, (B,), "seq_len")
+        self._struct = osprey_kv8(*key[1:9], self.max_pages, pages, t)
+        self._key = key
+        return self._struct
 
 
 def alloc_kv8(shape: DrafterShape, page_table: np.ndarray, n_pages: int, tail_pages: int = 2, device="cuda") -> Kv8Cache:
@@ -364,10 +377,11 @@ def _append_rows(ctx, B, n_rows, k_rows, v_rows, status, layer):
         raise ValueError("rows are [n_layers, total, Hkv, hd], or [total, Hkv, hd] of one layer")
     if layer is None and lead[0] != s.n_layers:
         raise ValueError(f"k_rows: {lead[0]} layers, expected {s.n_layers}")
-    inner = (s.n_kv_heads, s.head_dim)
-    stride = _strided_rows(k_rows, lead, inner, "k_rows")
-    if _strided_rows(v_rows, lead, inner, "v_rows") != stride or v_rows.dtype != k_rows.dtype:
-        raise ValueError("k_rows and v_rows must have the same type and spacing")
+    stride = _strided_rows(k_rows, lead, (s.n_kv_heads, s.head_dim), "k_rows")
+    if v_rows.dtype != k_rows.dtype or v_rows.shape != k_rows.shape or v_rows.get_device() != k_rows.get_device() or \
+            (v_rows.stride() != k_rows.stride() and
+             _strided_rows(v_rows, lead, (s.n_kv_heads, s.head_dim), "v_rows") != stride):
+        raise ValueError("v_rows must have the type, shape, device and spacing of k_rows")
     return lead[-1], stride
 
 

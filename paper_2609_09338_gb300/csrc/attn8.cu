@@ -16,11 +16,12 @@
 // float32, so no product of unlike sizes shares an accumulator.  bf16 queries are two
 // planes exactly.
 //
-// Per tile of 128 keys a thread is a key: it reads its scores from TMEM, the block
-// finds each query's running maximum, the thread writes its weights' planes, and the
-// output of the tile before, a thread now being a dim, is added from TMEM to registers
-// in float32.  The V block's scale goes into the weight: w' = 2^(s + log2(vs) - m'),
-// the sum adds w' / vs.
+// Per tile of 128 keys a thread is a key: it reads its scores from TMEM and writes its
+// weights' planes; then it is a dim, and adds the output of the tile before from TMEM to
+// registers in float32.  Weights are 2^(s - m) with a reference m that stays while no
+// score exceeds it by more than A8_OVER: then a tile needs one vote, and no maxima.
+// The V block's scale goes into the weight, w' = 2^(s + log2(vs) - m); the sum adds
+// w' / vs.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -34,25 +35,30 @@ namespace osp {
 
 namespace cg = cooperative_groups;
 
-constexpr int A8_C = 128;            // compute threads
-constexpr int A8_T = A8_C + 32;      // and the warp that copies and issues
 constexpr int A8_CH = 32;            // tail keys of a step
-constexpr float A8_LO = -40.f;       // smallest log2 of a V scale that moves the maximum (a8_scales)
+constexpr int A8_PCH = 144;          // bytes between the weights' core matrices: 128 and 4 banks, so that a warp's two do not meet
+constexpr float A8_LO = -40.f;       // smallest log2 of a V scale that moves the reference
+constexpr float A8_OVER = 4.f;       // a weight is at most 2^A8_OVER, times A8_UP an e4m3 number
+constexpr float A8_UP = 16.f;
 
-template <int HD_, int QT_, int QP_, int PP_, int BPS_>
+// QT queries a block, QW of them a warpgroup's (4 warps); QP and PP planes of a query and
+// of a weight; BPS blocks an SM, of NS slots of K and V each.
+template <int HD_, int QT_, int QW_, int QP_, int PP_, int BPS_, int NS_>
 struct A8 {
-    static constexpr int HD = HD_, QT = QT_, QP = QP_, PP = PP_, BPS = BPS_;
-    static constexpr int KB = 16 * HD, TB = 8 * KB;     // bytes of a page, of a tile's slot
-    static constexpr int NS = HD == 128 ? 2 : 4;        // slots of K and of V
-    static constexpr int SC = QP * QT, OC = PP * QT;    // TMEM columns of the scores, of the output
-    static constexpr int TM = 512 / BPS;                // columns a block may take
+    static constexpr int HD = HD_, QT = QT_, QW = QW_, QP = QP_, PP = PP_, BPS = BPS_, NS = NS_ * 128 / HD;
+    static constexpr int NWG = QT / QW, CT = NWG * 128;   // warpgroups that compute, their threads
+    static constexpr int THREADS = CT + 96;               // and three warps: products, K copies, V copies
+    static constexpr int KB = 16 * HD, TB = 8 * KB;       // bytes of a page, of a tile's slot
+    static constexpr int SC = (QP * QT + 15) / 16 * 16, OC = (PP * QT + 15) / 16 * 16;   // TMEM columns of scores, output
+    static constexpr int TM = 512 / BPS;                  // columns a block may take
     static constexpr int NSB = 2 * SC + OC <= TM ? 2 : 1;
-    static constexpr int COLS = NSB * SC + OC <= 32 ? 32 : NSB * SC + OC <= 64 ? 64 : NSB * SC + OC <= 128 ? 128
-                              : NSB * SC + OC <= 256 ? 256 : 512;
-    static constexpr int QB = SC * HD;                               // bytes of q's planes
-    static constexpr int PB = OC * 128 > QT * HD * 4 ? OC * 128 : QT * HD * 4;   // the weights' planes, or q for the tail
+    static constexpr int USED = NSB * SC + OC;
+    static constexpr int COLS = USED <= 32 ? 32 : USED <= 64 ? 64 : USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
+    static constexpr int QB = SC * HD;                    // bytes of q's planes
+    static constexpr int PW = 8 * A8_PCH * (OC / 8);         // bytes of the weights' planes
+    static constexpr int PB = PW > QT * HD * 4 ? PW : QT * HD * 4;   // their place, q's for the tail
     static constexpr int SMEM = 2 * NS * TB + QB + PB + QT * A8_CH * 4;
-    static_assert(COLS <= TM && SC % 16 == 0 && OC % 16 == 0 && QB + PB >= KB, "operands");
+    static_assert(COLS <= TM && QB + PB >= KB && QT % QW == 0, "operands");
     static_assert(QT * HD * 4 <= NS * TB, "the merge's outputs take the K slots");
 };
 
@@ -80,57 +86,111 @@ __device__ __forceinline__ float a8_warp_max(float x) {
 }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// TMEM columns [c0, c0 + P x QT) of the warp's lanes, plane by plane: x[q] = sum over planes of 16^-p column p QT + q
-template <int QT, int P>
-__device__ __forceinline__ void a8_planes(uint32_t col, float (&x)[QT]) {
-    if constexpr (QT == 8) {   // a load holds two planes
-        float v[P / 2][16];
-#pragma unroll
-        for (int c = 0; c < P / 2; ++c) tc_ld16(col + c * 16, v[c]);
-        tc_ld_wait();
-#pragma unroll
-        for (int c = 0; c < P / 2; ++c) tc_ld_tie(v[c]);
-#pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            float s = 0.f;
-#pragma unroll
-            for (int p = P - 1; p >= 0; --p) s = fmaf(s, 0.0625f, v[p / 2][(p & 1) * 8 + q]);
-            x[q] = s;
-        }
+template <int N>
+__device__ __forceinline__ void a8_ld(uint32_t addr, float *v) {
+    uint32_t r[N];
+    if constexpr (N == 4) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
     } else {
+        static_assert(N == 8, "columns");
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "r"(addr));
+    }
 #pragma unroll
-        for (int q = 0; q < QT; ++q) x[q] = 0.f;
+    for (int j = 0; j < N; ++j) v[j] = __uint_as_float(r[j]);
+}
+
+// Two floats an instruction.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 mk2(float x, float y) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void un2(f2 v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ f2 fma2(f2 x, f2 y, f2 z) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 x, f2 y) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 x, f2 y) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+
+// Planes of QW queries from TMEM column `col` on, QT columns a plane: x = sum over planes of 16^-p plane p, in pairs
+template <int QT, int QW, int P>
+__device__ __forceinline__ void a8_planes(uint32_t col, f2 (&x)[QW / 2]) {
+    float v[P][QW];
 #pragma unroll
-        for (int p = P - 1; p >= 0; --p) {
-            float v[QT / 16][16];
+    for (int p = 0; p < P; ++p) a8_ld<QW>(col + p * QT, v[p]);
+    tc_ld_wait();
 #pragma unroll
-            for (int c = 0; c < QT / 16; ++c) tc_ld16(col + p * QT + c * 16, v[c]);
-            tc_ld_wait();
+    for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int c = 0; c < QT / 16; ++c) tc_ld_tie(v[c]);
+        for (int q = 0; q < QW; ++q) asm volatile("" : "+f"(v[p][q]));   // not before the wait
+    const f2 sixteenth = mk2(0.0625f, 0.0625f);
 #pragma unroll
-            for (int q = 0; q < QT; ++q) x[q] = fmaf(x[q], 0.0625f, v[q / 16][q % 16]);
-        }
+    for (int q = 0; q < QW / 2; ++q) {
+        x[q] = mk2(v[P - 1][2 * q], v[P - 1][2 * q + 1]);
+#pragma unroll
+        for (int p = P - 2; p >= 0; --p) x[q] = fma2(x[q], sixteenth, mk2(v[p][2 * q], v[p][2 * q + 1]));
     }
 }
 
+// A barrier of a warpgroup that tells whether any thread's flag is set.
+__device__ __forceinline__ bool a8_vote(int id, bool x) {
+    uint32_t r;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, %2, 128, p;\nselp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(r) : "r"((uint32_t)x), "r"(id) : "memory");
+    return r != 0;
+}
+
+// Waits for a phase, about a second at most: then, or when another wait of the block has
+// run out, false.  A phase that has ended costs one instruction.
+__device__ __forceinline__ bool a8_wait(uint64_t *bar, uint32_t parity, int *abort, int32_t *status) {
+    long long t0 = 0;
+    for (int i = 0; !mbar_try_wait(bar, parity);) {
+        if (++i < 64) continue;
+        if (*(volatile int *)abort) return false;
+        const long long t = clock64();
+        if (!t0) t0 = t;
+        if (t - t0 > 2000000000LL) {
+            *(volatile int *)abort = 1;
+            set_status(status, OSPREY_ERR_TIMEOUT);
+            return false;
+        }
+        i = 0;
+    }
+    return true;
+}
+
 template <typename C>
-__global__ void __launch_bounds__(A8_T, C::BPS) attn8_kernel(const __grid_constant__ Attn8Args a, int tiles) {
-    constexpr int HD = C::HD, QT = C::QT, QP = C::QP, PP = C::PP, KB = C::KB, TB = C::TB, NS = C::NS;
+__global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_constant__ Attn8Args a, int tiles) {
+    constexpr int HD = C::HD, QT = C::QT, QW = C::QW, QP = C::QP, PP = C::PP, KB = C::KB, TB = C::TB, NS = C::NS, NSB = C::NSB;
+    constexpr int W_MMA = C::CT / 32, W_K = W_MMA + 1;   // the warps that do not compute: products, K copies, V copies
     extern __shared__ __align__(1024) uint8_t sm[];
     uint8_t *sk = sm, *sv = sk + NS * TB, *sqp = sv + NS * TB, *spp = sqp + C::QB;
     float *sq = (float *)spp;                       // [QT][HD] while the tail is read
     float *sp = (float *)(spp + C::PB);             // [QT][A8_CH] the tail's weights
     float *so = (float *)sk;                        // [QT][HD] at the end
-    __shared__ __align__(8) uint64_t kfull[NS], vfull[NS], sfull[2], pready, ofull;
-    __shared__ __align__(16) float s_red[2][4][QT], s_mul[QT];
-    __shared__ float s_m[QT], s_l[QT], s_corr[QT], s_lw[4][QT];
+    __shared__ __align__(8) uint64_t kfull[NS], vfull[NS], kfree[NS], vfree[NS], sfull[2], sread[1], pready, ofull;
+    __shared__ __align__(16) float s_red[C::NWG][4][QW], s_mul[QT], s_nref[QT], s_m[QT];
+    __shared__ float s_l[QT], s_corr[QT], s_lw[4][QT];
     __shared__ int s_pos[QT], s_bad, s_abort;
     __shared__ uint32_t s_tmem;
     cg::cluster_group cluster = cg::this_cluster();
     const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int unit = blockIdx.x / cs, kvh = unit % a.Hkv, tile = unit / a.Hkv % tiles, b = unit / a.Hkv / tiles;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.Hq / a.Hkv;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lg = __ffs(a.Hq / a.Hkv) - 1, G = 1 << lg;   // a power of two
     int nr, base, c8;
     bool ok = true;
     if (a.seq_len) {
@@ -149,91 +209,125 @@ __global__ void __launch_bounds__(A8_T, C::BPS) attn8_kernel(const __grid_consta
         base = a.map.pos0[b] + (a.map.step == 0 ? 0 : nn + a.map.step - 1);
         c8 = a.map.pos0[b] / 16;
     }
-    const int i0 = tile * QT, nq = min(QT, nr * G - i0);
+    const int i0 = tile * QT, nq = min(QT, nr * G - i0), nact = (nq + QW - 1) / QW;   // queries, warpgroups that have some
     if (nq <= 0) {   // the whole cluster
         pdl_wait();
         return;
     }
     // this block's finished pages; keys past the last query's position are seen by none
-    const int last = base + (i0 + nq - 1) / G;
+    const int last = base + ((i0 + nq - 1) >> lg);
     const int np_all = ok ? min(c8, last / 16 + 1) : 0, per = (np_all + cs - 1) / cs;
     const int pg0 = min(np_all, rank * per), np = min(np_all, pg0 + per) - pg0, nt = (np + 7) / 8;
     const int32_t *tab = a.page_table + (size_t)b * a.max_pages + pg0;
-    auto page_of = [&](int p) {   // page p of the range as a block's number, 0 for a bad id
-        const int id = __ldg(tab + p);
+    // a block's number of a page id; a bad id is noted and read as page 0 (the check waits for the id, so it comes at its use)
+    bool bad_id = false;
+    auto block_of = [&](int id) {
         const bool good = id >= 0 && id < a.n_pages;
-        if (!good) s_bad = 1;
+        bad_id |= !good;
         return (size_t)(good ? id : 0) * a.Hkv + kvh;
     };
-    if (tid == A8_C) {
-        for (int i = 0; i < NS; ++i) {
-            mbar_init(&kfull[i], 1);
-            mbar_init(&vfull[i], 1);
+    // Copies of a tile's K or V pages from the page ids that lanes 0 .. 7 hold, issued by one
+    // lane: a copy takes a warp some 130 cycles to issue, whichever lane's, so K and V have
+    // a warp each (one warp for both, and for the products: 3500 cycles a tile).
+    uint8_t *const ring = warp == W_K ? sk : sv;
+    uint64_t *const full = warp == W_K ? kfull : vfull, *const freed = warp == W_K ? kfree : vfree;
+    auto load = [&](int t, int id) {
+        const int n = min(8, np - t * 8), slot = t % NS;
+        const unsigned long long at = (unsigned long long)((warp == W_K ? a.k8 : a.v8) + block_of(id) * KB);
+        unsigned long long from[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) from[p] = __shfl_sync(0xffffffffu, at, p);
+        if (tc_elect()) {
+            mbar_arrive_expect_tx(&full[slot], (uint32_t)(n * KB));
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (p < n) bulk_g2s(ring + slot * TB + p * KB, (const void *)from[p], KB, &full[slot]);
         }
-        mbar_init(&sfull[0], 1);
-        mbar_init(&sfull[1], 1);
-        mbar_init(&ofull, 1);
-        mbar_init(&pready, 4);
-        s_bad = !ok;
-        s_abort = 0;
-        mbar_fence_init();
-    }
-    if (warp == 4) {
+        __syncwarp();
+    };
+    auto lane_id = [&](int t) { return lane < 8 && t * 8 + lane < np ? __ldg(tab + t * 8 + lane) : 0; };
+    int ids = 0;   // of the next tile to ask for
+    if (warp == W_MMA) {
+        if (lane == 0) {
+            mbar_init(&sfull[0], 1);
+            mbar_init(&sfull[1], 1);
+            mbar_init(sread, 4 * nact);
+            mbar_init(&ofull, 1);
+            mbar_init(&pready, 4 * nact);
+            s_bad = !ok;
+            s_abort = 0;
+            mbar_fence_init();
+        }
         __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)),
                      "r"((uint32_t)C::COLS));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
-    // copies of a tile's K or V pages, a lane a page
-    auto load = [&](int t, uint8_t *ring, const uint8_t *src, size_t blk, uint64_t *full) {
-        const int n = min(8, np - t * 8), slot = t % NS;
-        if (lane == 0) mbar_arrive_expect_tx(&full[slot], (uint32_t)(n * KB));
-        __syncwarp();
-        if (lane < n) bulk_g2s(ring + slot * TB + lane * KB, src + blk * KB, KB, &full[slot]);
-    };
-    size_t blk_k = 0, blk_v = 0;   // control warp: the lane's page of the next K tile, of the next V tile
-    auto lane_page = [&](int t) { return lane < 8 && t * 8 + lane < np ? page_of(t * 8 + lane) : (size_t)0; };
-    if (warp == 4) {
-        // finished pages are written by no kernel that this one may overlap
-        for (int t = 0; t < min(NS, nt); ++t) {
-            const size_t blk = lane_page(t);
-            load(t, sk, a.k8, blk, kfull);
-            load(t, sv, a.v8, blk, vfull);
+    } else if (warp >= W_K) {
+        int first[NS];
+#pragma unroll
+        for (int t = 0; t < NS; ++t) first[t] = lane_id(t);
+        ids = lane_id(NS);
+        if (lane == 0) {
+            for (int i = 0; i < NS; ++i) {
+                mbar_init(&full[i], 1);
+                mbar_init(&freed[i], 1);
+            }
+            mbar_fence_init();
         }
-        blk_k = lane_page(NS);
+        __syncwarp();
+        // finished pages are written by no kernel that this one may overlap
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+            if (t < nt) load(t, first[t]);
     }
-    pdl_wait();   // queries and the tail's rows
+    // compute threads: the thread's key of tile t; its page's scales are loaded a tile ahead, the page's id two
+    const int wt = tid & 127;
+    float ksn = 0.f, vsn = 1.f;
+    auto key_id = [&](int t) { return t * 8 + (wt >> 4) < np ? __ldg(tab + t * 8 + (wt >> 4)) : 0; };
+    auto scales = [&](int t) {
+        if (t * 8 + (wt >> 4) < np) {
+            const size_t blk = block_of(ids);
+            ksn = __ldg(a.k_scale + blk);
+            vsn = __ldg(a.v_scale + blk);
+        }
+    };
     const bool tail = ok && rank == cs - 1;
-    if (warp < 4) {
+    if (warp < W_MMA) {
+        ids = key_id(0);
+        if (!a.seq_len) pdl_wait();   // queries and the tail's rows come from a draft call's kernels
         // queries: rotated, scaled to a magnitude of 128 to 256, split into planes; a lane holds pairs (d, d + HD / 2)
-        constexpr int NP = HD / 64;
-        for (int q = warp; q < QT; q += 4) {
-            const int i = min(i0 + q, i0 + nq - 1), j = i / G, g = i - j * G;   // queries past the last one are copies of it
+        constexpr int NP = HD / 64, PER = (QT + W_MMA - 1) / W_MMA;
+        float xs[PER][2 * NP];
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int q = warp + u * W_MMA, i = min(i0 + q, a.max_rows * G - 1), j = i >> lg, g = i & (G - 1);
             const int64_t at = ((int64_t)b * a.max_rows + j) * a.q_stride + (kvh * G + g) * HD + lane;
-            float x[2 * NP], mag = 0.f;
+#pragma unroll
+            for (int k = 0; k < 2 * NP; ++k) {
+                const int64_t e = at + 32 * (k % NP) + (k / NP) * (HD / 2);
+                xs[u][k] = q >= nq ? 0.f : a.q_f32 ? ((const float *)a.q)[e] : bf_to_f(((const uint16_t *)a.q)[e]);
+            }
+        }
+        scales(0);
+        ids = key_id(1);
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int q = warp + u * W_MMA, j = (i0 + q) >> lg;
+            if (q >= QT) break;
+            float (&x)[2 * NP] = xs[u];
+            float mag = 0.f;
             bool fin = true;
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
-                const int d = lane + 32 * k;
-                float u, w;
-                if (a.q_f32) {
-                    u = ((const float *)a.q)[at + 32 * k];
-                    w = ((const float *)a.q)[at + 32 * k + HD / 2];
-                } else {
-                    u = bf_to_f(((const uint16_t *)a.q)[at + 32 * k]);
-                    w = bf_to_f(((const uint16_t *)a.q)[at + 32 * k + HD / 2]);
-                }
                 if (a.rotate) {
                     float c, s;
-                    rope_cs_fix(a.freq[d], base + j, c, s);
-                    const float t = u * c - w * s;
-                    w = w * c + u * s;
-                    u = t;
+                    rope_cs_fix(a.freq[lane + 32 * k], base + j, c, s);
+                    const float t = x[k] * c - x[NP + k] * s;
+                    x[NP + k] = x[NP + k] * c + x[k] * s;
+                    x[k] = t;
                 }
-                x[k] = u;
-                x[NP + k] = w;
-                fin = fin && isfinite(u) && isfinite(w);
-                mag = fmaxf(mag, fmaxf(fabsf(u), fabsf(w)));
+                fin = fin && isfinite(x[k]) && isfinite(x[NP + k]);
+                mag = fmaxf(mag, fmaxf(fabsf(x[k]), fabsf(x[NP + k])));
             }
             mag = a8_warp_max(mag);
             fin = __all_sync(0xffffffffu, fin);
@@ -257,104 +351,111 @@ __global__ void __launch_bounds__(A8_T, C::BPS) attn8_kernel(const __grid_consta
                 s_mul[q] = fin ? unit * kv8_pow2(-e) : __uint_as_float(0x7fffffffu);
                 s_pos[q] = base + j;
                 s_m[q] = -INFINITY;
+                s_nref[q] = 0.f;
                 s_l[q] = 0.f;
             }
         }
         fence_async_smem();
     }
+    if (a.seq_len || warp >= W_MMA) pdl_wait();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     // not before this block holds its TMEM: a dependent's blocks take theirs and wait for this kernel
     pdl_trigger();
-    const uint32_t tmem = s_tmem, tm_o = tmem + C::NSB * C::SC;
+    const uint32_t tmem = s_tmem, tm_o = tmem + NSB * C::SC;
     // After a wait that ran out nothing is waited for or issued any more: the loops run to
     // their ends, and the cluster's outputs are 0.
-    auto wait = [&](uint64_t *bar, int phase) {
-        if (!*(volatile int *)&s_abort && !mbar_wait(bar, (uint32_t)phase & 1)) {
-            s_abort = 1;
-            set_status(a.status, OSPREY_ERR_TIMEOUT);
-        }
+    auto wait1 = [&](uint64_t *bar, uint32_t phase) { return a8_wait(bar, phase & 1, &s_abort, a.status); };
+    auto wait = [&](uint64_t *bar, uint32_t phase) {
+        wait1(bar, phase);
         __syncwarp();
     };
-    if (warp == 4) {
-        auto scores = [&](int t) {   // scores of tile t, 128 keys x (planes x queries)
-            wait(&kfull[t % NS], t / NS);
-            if (lane == 0 && !s_abort) {
+    float keep[QW];   // a block alone: its outputs
+    auto stop = [&] { return __shfl_sync(0xffffffffu, *(volatile int *)&s_abort, 0) != 0; };
+    if (warp == W_MMA) {
+        // One lane issues the products, slots and descriptors by increments: with the whole
+        // warp in the loop, slots by division, a tile's two products took 1750 cycles to issue.
+        if (tc_elect()) {
+            const uint64_t dK = a8_desc(smem_u32(sk), 128, HD * 8), dQ = a8_desc(smem_u32(sqp), 128, HD * 8);
+            const uint64_t dV = a8_desc(smem_u32(sv), KB, 128), dP = a8_desc(smem_u32(spp), A8_PCH, 8 * A8_PCH);
+            int ks = 0, kph = 0, vs = 0, vph = 0;   // slots and their phases
+            auto scores = [&](int t) {   // of tile t: 128 keys x (planes x queries)
+                const int sb = NSB == 2 ? t & 1 : 0;
+                if (!wait1(&kfull[ks], kph)) return false;
+                // the columns' last readers have read them (two score buffers: before the weights of tile t - 2 were written)
+                if (NSB == 1 && t > 0 && !wait1(sread, t - 1)) return false;
                 tc_fence_after();
-                const uint32_t A = smem_u32(sk + t % NS * TB), Q = smem_u32(sqp);
 #pragma unroll
                 for (int k = 0; k < HD / 32; ++k)
-                    a8_mma(tmem + (C::NSB == 2 ? (t & 1) * C::SC : 0), a8_desc(A + k * 256, 128, HD * 8),
-                           a8_desc(Q + k * 256, 128, HD * 8), a8_idesc(C::SC), k > 0);
-                tc_commit(&sfull[C::NSB == 2 ? t & 1 : 0]);
-            }
-            __syncwarp();
-        };
-        auto output = [&](int t) {   // head_dim x (planes x queries) over tile t's keys
-            wait(&pready, t);   // its weights are written; its scores are read, the output of the tile before too
-            wait(&vfull[t % NS], t / NS);
-            if (lane == 0 && !s_abort) {
+                    a8_mma(tmem + sb * C::SC, dK + (ks * TB + k * 256) / 16, dQ + k * 16, a8_idesc(C::SC), k > 0);
+                tc_commit(&sfull[sb]);
+                tc_commit(&kfree[ks]);
+                if (++ks == NS) ks = 0, kph ^= 1;
+                return true;
+            };
+            bool go = nt > 0 && scores(0);
+            for (int t = 0; t < nt && go; ++t) {
+                if (t + 1 < nt) go = scores(t + 1);
+                // head_dim x (planes x queries) over tile t's keys, when its weights are written and the output before is read
+                go = go && wait1(&vfull[vs], vph) && wait1(&pready, t);
+                if (!go) break;
                 tc_fence_after();
-                const uint32_t A = smem_u32(sv + t % NS * TB), P = smem_u32(spp);
-                const int n = min(8, np - t * 8);
-                for (int k = 0; k < (n + 1) / 2; ++k)
-                    a8_mma(tm_o, a8_desc(A + k * 2 * KB, KB, 128), a8_desc(P + k * 256, 128, 1024), a8_idesc(C::OC), k > 0);
-                tc_commit(&ofull);
-            }
-            if (__shfl_sync(0xffffffffu, *(volatile int *)&s_abort, 0)) return;
-            if (t >= 1 && t - 1 + NS < nt) load(t - 1 + NS, sv, a.v8, blk_v, vfull);   // the slot of tile t - 1
-            if (t + NS < nt) {
-                load(t + NS, sk, a.k8, blk_k, kfull);
-                blk_v = blk_k;
-                blk_k = lane_page(t + NS + 1);
-            }
-        };
-        for (int t = 0; t <= nt && nt > 0; ++t) {
-            if (C::NSB == 2 && t < nt) scores(t);
-            if (t > 0) output(t - 1);
-            if (C::NSB == 1 && t < nt) scores(t);
-            if (__shfl_sync(0xffffffffu, *(volatile int *)&s_abort, 0)) break;
-        }
-        if (s_abort)   // let what is on its way land before the block ends
-            for (int i = 0; i < NS; ++i)
-                for (int ph = 0; ph < 2; ++ph) {
-                    mbar_wait(&kfull[i], ph, 20000000LL);
-                    mbar_wait(&vfull[i], ph, 20000000LL);
-                }
-    } else {
-        float o[QT], l[QT], m[QT];
+                const int n = (np - t * 8 + 1) / 2;
+                if (n >= 4) {
 #pragma unroll
-        for (int q = 0; q < QT; ++q) o[q] = 0.f;
+                    for (int k = 0; k < 4; ++k)
+                        a8_mma(tm_o, dV + (vs * TB + k * 2 * KB) / 16, dP + k * (2 * A8_PCH / 16), a8_idesc(C::OC), k > 0);
+                } else
+                    for (int k = 0; k < n; ++k) a8_mma(tm_o, dV + (vs * TB + k * 2 * KB) / 16, dP + k * (2 * A8_PCH / 16), a8_idesc(C::OC), k > 0);
+                tc_commit(&ofull);
+                tc_commit(&vfree[vs]);
+                if (++vs == NS) vs = 0, vph ^= 1;
+            }
+        }
+        __syncwarp();
+    } else if (warp >= W_K) {
+        for (int t = 0; t + NS < nt; ++t) {   // a slot is asked for again when the product that read it has ended
+            wait(&freed[t % NS], t / NS);
+            if (stop()) break;
+            load(t + NS, ids);
+            ids = lane_id(t + NS + 1);
+        }
+    } else if (warp < 4 * nact) {   // the columns of a warpgroup without queries hold anything, and nobody reads them
+        const int wg = warp / 4, ww = warp % 4, q0 = wg * QW, bar = 1 + wg;   // this warpgroup's queries and barrier
+        float o[QW];
+#pragma unroll
+        for (int q = 0; q < QW; ++q) o[q] = 0.f;
         if (tail)   // bf16 rows behind the finished pages, in float32
             for (int key0 = c8 * 16; key0 <= last; key0 += A8_CH) {
                 const int key1 = min(last + 1, key0 + A8_CH);
                 // a key is four lanes': every fourth group of 4 dims
-                const int key = key0 + tid / 4, quarter = tid % 4;
-                float s[QT];
+                const int key = key0 + wt / 4, quarter = wt % 4;
+                float s[QW];
 #pragma unroll
-                for (int q = 0; q < QT; ++q) s[q] = 0.f;
+                for (int q = 0; q < QW; ++q) s[q] = 0.f;
                 if (key < key1) {
                     const uint16_t *kr = a.k_tail +
                                          (((size_t)b * a.tail_pages + key / 16 % a.tail_pages) * a.Hkv + kvh) * 16 * HD + (key % 16) * HD;
+#pragma unroll 2
                     for (int d = quarter * 4; d < HD; d += 16) {
                         const uint2 w = *(const uint2 *)(kr + d);
                         const float f0 = bf_lo(w.x), f1 = bf_hi(w.x), f2 = bf_lo(w.y), f3 = bf_hi(w.y);
 #pragma unroll
-                        for (int q = 0; q < QT; ++q) {
-                            const float4 u = *(const float4 *)&sq[q * HD + d];
+                        for (int q = 0; q < QW; ++q) {
+                            const float4 u = *(const float4 *)&sq[(q0 + q) * HD + d];
                             s[q] = fmaf(u.x, f0, fmaf(u.y, f1, fmaf(u.z, f2, fmaf(u.w, f3, s[q]))));
                         }
                     }
                 }
 #pragma unroll
-                for (int q = 0; q < QT; ++q) {
+                for (int q = 0; q < QW; ++q) {
                     s[q] += __shfl_xor_sync(0xffffffffu, s[q], 1);
                     s[q] += __shfl_xor_sync(0xffffffffu, s[q], 2);
-                    if (quarter == 0) sp[q * A8_CH + tid / 4] = s[q];
+                    if (quarter == 0) sp[(q0 + q) * A8_CH + wt / 4] = s[q];
                 }
-                named_sync(1, A8_C);
-                for (int q = warp; q < QT; q += 4) {
+                named_sync(bar, 128);
+                for (int q = q0 + ww; q < q0 + QW; q += 4) {
                     const bool see = key0 + lane < key1 && key0 + lane <= s_pos[q];
                     const float x = see ? sp[q * A8_CH + lane] : -INFINITY;
                     const float mn = fmaxf(s_m[q], warp_max(x)), ref = mn == -INFINITY ? 0.f : mn;
@@ -366,118 +467,140 @@ __global__ void __launch_bounds__(A8_T, C::BPS) attn8_kernel(const __grid_consta
                         s_corr[q] = corr;
                         s_l[q] = s_l[q] * corr + ls;
                         s_m[q] = mn;
+                        s_nref[q] = -ref;
                     }
                 }
-                named_sync(1, A8_C);
-                if (tid < HD) {
+                named_sync(bar, 128);
+                if (wt < HD) {
 #pragma unroll
-                    for (int q = 0; q < QT; ++q) o[q] *= s_corr[q];
+                    for (int q = 0; q < QW; ++q) o[q] *= s_corr[q0 + q];
                     for (int k = 0; k < key1 - key0; ++k) {
                         const int kk = key0 + k;
                         const float v = bf_to_f(a.v_tail[(((size_t)b * a.tail_pages + kk / 16 % a.tail_pages) * a.Hkv + kvh) * 16 * HD +
-                                                         (kk % 16) * HD + tid]);
+                                                         (kk % 16) * HD + wt]);
 #pragma unroll
-                        for (int q = 0; q < QT; ++q) {
-                            const float p = sp[q * A8_CH + k];
+                        for (int q = 0; q < QW; ++q) {
+                            const float p = sp[(q0 + q) * A8_CH + k];
                             if (!(p < 0.f)) o[q] = fmaf(p, v, o[q]);
                         }
                     }
                 }
-                named_sync(1, A8_C);
+                named_sync(bar, 128);
             }
+        if (C::NWG > 1 && tail) named_sync(15, 128 * nact);   // every warpgroup has read q, whose place the weights take
+        constexpr int QH = QW / 2;
+        f2 o2[QH], l2[QH];   // pairs of queries
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            m[q] = s_m[q];
-            l[q] = tid == 0 ? s_l[q] : 0.f;
+        for (int q = 0; q < QH; ++q) {
+            o2[q] = mk2(o[2 * q], o[2 * q + 1]);
+            l2[q] = wt == 0 ? mk2(s_l[q0 + 2 * q], s_l[q0 + 2 * q + 1]) : 0ull;
         }
-        // the thread's key of tile t: its page's scales are loaded a tile ahead
-        float ks = 0.f, vs = 1.f, ksn = 0.f, vsn = 1.f;
-        auto scales = [&](int t, float &k, float &v) {
-            const int p = t * 8 + (tid >> 4);
-            if (p < np) {
-                const size_t blk = page_of(p);
-                k = __ldg(a.k_scale + blk);
-                v = __ldg(a.v_scale + blk);
-            }
-        };
-        scales(0, ksn, vsn);
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        const int first_pos = base + i0 / G;
+        const uint32_t lanes = (uint32_t)(ww * 32) << 16;
+        const int first_pos = base + (i0 >> lg);
+        const f2 down = mk2(1.f / A8_UP, 1.f / A8_UP), sixteen = mk2(16.f, 16.f), minus = mk2(-16.f, -16.f);
         for (int t = 0; t < nt; ++t) {
-            ks = ksn;
-            vs = vsn;
-            scales(t + 1, ksn, vsn);
-            const int n = min(8, np - t * 8), key = (pg0 + t * 8) * 16 + tid;
-            // a scale under 2^A8_LO (a block of zeros) would push the weight out of float32's range
-            const float lv = __log2f(vs), lvs = lv < A8_LO ? A8_LO : lv;
+            const float ks = ksn, vs = vsn;
+            scales(t + 1);
+            ids = key_id(t + 2);
+            const int n = min(8, np - t * 8), key = (pg0 + t * 8) * 16 + wt;
+            // a scale under 2^A8_LO (a block of zeros) would push the weight out of float32's range;
             // a NaN scale comes through the score, to the queries that see the key alone
-            const float rvs = lv < A8_LO ? a8_ex2(-A8_LO) : isnan(vs) ? 1.f : 1.f / vs, fvs = lv < A8_LO ? vs * a8_ex2(-A8_LO) : 1.f;
-            float s[QT];
-            if (C::NSB == 2) wait(&sfull[t & 1], t >> 1);
-            else wait(&sfull[0], t);
-            tc_fence_after();
-            a8_planes<QT, QP>(tmem + lanes + (C::NSB == 2 ? (t & 1) * C::SC : 0), s);
-            const bool in = tid < n * 16;
-            const bool whole = (pg0 + t * 8 + n) * 16 - 1 <= first_pos;   // every query sees the tile
-#pragma unroll
-            for (int q = 0; q < QT; ++q) s[q] = in ? fmaf(s[q] * ks, s_mul[q], lvs) : -INFINITY;
-            if (!whole)
-#pragma unroll
-                for (int q = 0; q < QT; ++q)
-                    if (key > s_pos[q]) s[q] = -INFINITY;
-            float4 mx[QT / 4];
-#pragma unroll
-            for (int q = 0; q < QT; ++q) ((float *)mx)[q] = a8_warp_max(s[q]);
-            if (lane == 0)
-#pragma unroll
-                for (int q = 0; q < QT; q += 4) *(float4 *)&s_red[t & 1][warp][q] = mx[q / 4];
-            named_sync(1, A8_C);
-            float corr[QT];
-#pragma unroll
-            for (int q = 0; q < QT; q += 4) {
-                float4 v[4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) v[w] = *(const float4 *)&s_red[t & 1][w][q];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    auto at = [&](const float4 &f) { return e == 0 ? f.x : e == 1 ? f.y : e == 2 ? f.z : f.w; };
-                    const float mn = fmaxf(fmaxf(m[q + e], fmaxf(at(v[0]), at(v[1]))), fmaxf(at(v[2]), at(v[3])));
-                    corr[q + e] = mn == -INFINITY ? 1.f : a8_ex2(m[q + e] - mn);
-                    m[q + e] = mn;
-                    l[q + e] *= corr[q + e];
-                }
+            float lvs, rvs;
+            asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lvs) : "f"(vs));
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rvs) : "f"(vs));
+            float fvs = A8_UP;
+            if (!(lvs >= A8_LO)) {
+                fvs = lvs < A8_LO ? vs * 0x1p40f * A8_UP : A8_UP;
+                rvs = lvs < A8_LO ? 0x1p40f : 1.f;
+                lvs = lvs < A8_LO ? A8_LO : lvs;
             }
+            f2 e2[QH];   // log2 of the weights
+            wait(&sfull[t % NSB], t / NSB);
+            tc_fence_after();
+            a8_planes<QT, QW, QP>(tmem + lanes + t % NSB * C::SC + q0, e2);
+            tc_fence_before();
+            __syncwarp();
+            if (NSB == 1 && lane == 0) mbar_arrive(sread);
+            const f2 ks2 = mk2(ks, ks), lv2 = mk2(lvs, lvs);
+            float e[QW];
+#pragma unroll
+            for (int q = 0; q < QH; q += 2) {
+                const ulonglong2 mu = *(const ulonglong2 *)&s_mul[q0 + 2 * q], rf = *(const ulonglong2 *)&s_nref[q0 + 2 * q];
+                e2[q] = fma2(e2[q], mul2(mu.x, ks2), add2(lv2, rf.x));
+                e2[q + 1] = fma2(e2[q + 1], mul2(mu.y, ks2), add2(lv2, rf.y));
+            }
+#pragma unroll
+            for (int q = 0; q < QH; ++q) un2(e2[q], e[2 * q], e[2 * q + 1]);
+            if ((pg0 + t * 8 + n) * 16 - 1 > first_pos || n < 8) {   // a key that is no one's, or not every query's
+                const bool in = wt < n * 16;
+#pragma unroll
+                for (int q = 0; q < QW; ++q)
+                    if (!in || key > s_pos[q0 + q]) e[q] = -INFINITY;
+            }
+            // the first tile sets the references too (the tail's may be far below)
+            float top = e[0];
+#pragma unroll
+            for (int q = 1; q < QW; ++q) top = fmaxf(top, e[q]);
+            const bool over = a8_vote(bar, top > (t == 0 ? -INFINITY : A8_OVER));
             if (t > 0) {   // the output of the tile before: a thread is a dim
                 wait(&ofull, t - 1);
                 tc_fence_after();
-                float x[QT];
-                a8_planes<QT, PP>(tm_o + lanes, x);
+                f2 x[QH];
+                a8_planes<QT, QW, PP>(tm_o + lanes + q0, x);
 #pragma unroll
-                for (int q = 0; q < QT; ++q) o[q] = (o[q] + x[q] * 0x1p-8f) * corr[q];
-            } else {
-#pragma unroll
-                for (int q = 0; q < QT; ++q) o[q] *= corr[q];
+                for (int q = 0; q < QH; ++q) o2[q] = fma2(x[q], down, o2[q]);
             }
-            // weights, times 256 as planes
-            uint8_t *dst = spp + (tid >> 4) * 128 + (tid & 15);
+            if (over) {   // new references: the tile's maxima, where they are above
 #pragma unroll
-            for (int q = 0; q < QT; q += 2) {
-                float x[2];
+                for (int q = 0; q < QW; ++q) {
+                    const float x = a8_warp_max(e[q]);
+                    if (lane == 0) s_red[wg][ww][q] = x;
+                }
+                named_sync(bar, 128);
+                float to[QW], corr[QW];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float p = a8_ex2(s[q + e] - (m[q + e] == -INFINITY ? 0.f : m[q + e]));
-                    l[q + e] = fmaf(p, rvs, l[q + e]);
-                    x[e] = p * fvs * 256.f;
+                for (int q = 0; q < QW; ++q) {
+                    const float x = fmaxf(fmaxf(s_red[wg][0][q], s_red[wg][1][q]), fmaxf(s_red[wg][2][q], s_red[wg][3][q]));
+                    const float m = s_m[q0 + q], ref = -s_nref[q0 + q];
+                    to[q] = fmaxf(m, ref + x);
+                    corr[q] = to[q] == -INFINITY ? 1.f : m == -INFINITY ? 0.f : a8_ex2(m - to[q]);
+                    if (to[q] != -INFINITY) e[q] -= to[q] - ref;
                 }
 #pragma unroll
+                for (int q = 0; q < QH; ++q) {
+                    const f2 c = mk2(corr[2 * q], corr[2 * q + 1]);
+                    l2[q] = mul2(l2[q], c);
+                    o2[q] = mul2(o2[q], c);
+                }
+                named_sync(bar, 128);   // the old references are read
+#pragma unroll
+                for (int q = 0; q < QW; ++q)
+                    if (wt == q) {
+                        s_m[q0 + q] = to[q];
+                        s_nref[q0 + q] = to[q] == -INFINITY ? 0.f : -to[q];
+                    }
+                named_sync(bar, 128);
+            }
+            // weights, as planes
+            uint8_t *dst = spp + (wt >> 4) * A8_PCH + (wt & 15);
+            const f2 rv2 = mk2(rvs, rvs), fv2 = mk2(fvs, fvs);
+#pragma unroll
+            for (int q = 0; q < QH; ++q) {
+                f2 x = mk2(a8_ex2(e[2 * q]), a8_ex2(e[2 * q + 1]));
+                l2[q] = fma2(x, rv2, l2[q]);
+                x = mul2(x, fv2);
+#pragma unroll
                 for (int p = 0; p < PP; ++p) {
-                    const int r = p * QT + q;
-                    const uint32_t c = e4m3x2(x[0], x[1]);
-                    dst[(r >> 3) * 1024 + (r & 7) * 16] = (uint8_t)c;
-                    dst[(r >> 3) * 1024 + (r & 7) * 16 + 16] = (uint8_t)(c >> 8);
-                    const float2 f = e4m3x2_f(c);
-                    x[0] = (x[0] - f.x) * 16.f;
-                    x[1] = (x[1] - f.y) * 16.f;
+                    const int r = p * QT + q0 + 2 * q;
+                    float x0, x1;
+                    un2(x, x0, x1);
+                    const uint32_t c = e4m3x2(x0, x1);
+                    dst[(r >> 3) * (8 * A8_PCH) + (r & 7) * 16] = (uint8_t)c;
+                    dst[(r >> 3) * (8 * A8_PCH) + (r & 7) * 16 + 16] = (uint8_t)(c >> 8);
+                    if (p + 1 < PP) {
+                        const float2 f = e4m3x2_f(c);
+                        x = fma2(mk2(f.x, f.y), minus, mul2(x, sixteen));
+                    }
                 }
             }
             // an odd number of pages: the reduction's last 16 keys are no one's, and 0 x anything has to be 0
@@ -490,59 +613,88 @@ __global__ void __launch_bounds__(A8_T, C::BPS) attn8_kernel(const __grid_consta
         if (nt > 0) {
             wait(&ofull, nt - 1);
             tc_fence_after();
-            float x[QT];
-            a8_planes<QT, PP>(tm_o + lanes, x);
+            f2 x[QH];
+            a8_planes<QT, QW, PP>(tm_o + lanes + q0, x);
 #pragma unroll
-            for (int q = 0; q < QT; ++q) o[q] = fmaf(x[q], 0x1p-8f, o[q]);
+            for (int q = 0; q < QH; ++q) o2[q] = fma2(x[q], down, o2[q]);
         }
+        float l[QW];
+#pragma unroll
+        for (int q = 0; q < QH; ++q) {
+            un2(o2[q], o[2 * q], o[2 * q + 1]);
+            un2(l2[q], l[2 * q], l[2 * q + 1]);
+        }
+        if (s_abort && tid == 0)   // let what is on its way land before the slots are written
+            for (int i = 0; i < NS; ++i)
+                for (int ph = 0; ph < 2; ++ph) {
+                    mbar_wait(&kfull[i], ph, 20000000LL);
+                    mbar_wait(&vfull[i], ph, 20000000LL);
+                }
         tc_fence_before();
-        // the block's partial: every MMA has ended, the K slots take the outputs
+        // the block's partial: every product has ended, the K slots take the outputs
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            const float x = warp_sum(l[q]);
-            if (lane == 0) s_lw[warp][q] = x;
-            if (tid < HD) so[q * HD + tid] = o[q];
-            if (tid == 0) s_m[q] = m[q];
-        }
-        named_sync(1, A8_C);
-        if (tid < QT) s_l[tid] = s_lw[0][tid] + s_lw[1][tid] + s_lw[2][tid] + s_lw[3][tid];
-        if (tid == 0) {
-            if (s_bad && ok) set_status(a.status, OSPREY_ERR_CAPACITY);
-            if (s_abort) s_bad = 1;
-        }
+        for (int q = 0; q < QW; ++q)
+            if (wt < HD && cs > 1) so[(q0 + q) * HD + wt] = o[q];
+        // the warp's sums: lanes hand half of their queries to one another until each has one
+#pragma unroll
+        for (int h = QW / 2, d = 16; h >= 1; h /= 2, d /= 2)
+#pragma unroll
+            for (int q = 0; q < h; ++q) {
+                const bool up = lane & d;
+                const float x = __shfl_xor_sync(0xffffffffu, up ? l[q] : l[q + h], d);
+                l[q] = (up ? l[q + h] : l[q]) + x;
+            }
+#pragma unroll
+        for (int d = 16 / QW; d >= 1; d /= 2) l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+        if (lane % (32 / QW) == 0) s_lw[ww][q0 + lane / (32 / QW)] = l[0];
+        named_sync(bar, 128);
+        if (wt < QW) s_l[q0 + wt] = s_lw[0][q0 + wt] + s_lw[1][q0 + wt] + s_lw[2][q0 + wt] + s_lw[3][q0 + wt];
+        if (tid == 0 && s_abort) s_bad = 1;
+#pragma unroll
+        for (int q = 0; q < QW; ++q) keep[q] = o[q];
     }
+    if (bad_id) {
+        s_bad = 1;
+        set_status(a.status, OSPREY_ERR_CAPACITY);
+    }
+    auto store = [&](int q, float y) {   // dim wt of query q
+        const int i = i0 + q, j = i >> lg, col = (kvh * G + (i & (G - 1))) * HD + wt;
+        const size_t at = ((size_t)b * a.max_rows + j) * a.Hq * HD + col;
+        if (a.planes.q) attn_store(a.planes, b * a.max_rows + j, col, y);
+        else if (a.q_f32) ((float *)a.out)[at] = y;
+        else ((uint16_t *)a.out)[at] = (uint16_t)kv8_bf2(y, 0.f);
+    };
     __syncwarp();
-    cluster.sync();
-    if (warp == 4) {
+    if (cs > 1) cluster.sync();
+    else __syncthreads();
+    if (warp == W_MMA) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::COLS));
-    } else {
-        for (int q = rank; q < nq; q += cs) {
-            float M = -INFINITY;
-            bool bad = false;
-            for (int r = 0; r < cs; ++r) {
-                M = fmaxf(M, *cluster.map_shared_rank(&s_m[q], r));
-                bad |= *cluster.map_shared_rank(&s_bad, r) != 0;
-            }
-            float num = 0.f, den = 0.f;
-            for (int r = 0; r < cs; ++r) {
-                const float mr = *cluster.map_shared_rank(&s_m[q], r), lr = *cluster.map_shared_rank(&s_l[q], r);
-                if (mr == -INFINITY && !isnan(lr)) continue;
-                const float f = mr == -INFINITY ? 0.f : a8_ex2(mr - M);
-                den = fmaf(f, lr, den);
-                if (tid < HD) num = fmaf(f, *cluster.map_shared_rank(&so[q * HD + tid], r), num);
-            }
-            if (tid < HD) {
-                const int j = (i0 + q) / G, col = (kvh * G + (i0 + q) % G) * HD + tid;
-                const float y = bad ? 0.f : num / den;
-                const size_t at = ((size_t)b * a.max_rows + j) * a.Hq * HD + col;
-                if (a.planes.q) attn_store(a.planes, b * a.max_rows + j, col, y);
-                else if (a.q_f32) ((float *)a.out)[at] = y;
-                else ((uint16_t *)a.out)[at] = (uint16_t)kv8_bf2(y, 0.f);
-            }
+    } else if (warp < W_MMA) {
+        // lane r holds what rank r left of a query; a thread is a dim of the output
+        if (cs == 1 && wt < HD && warp < 4 * nact) {
+#pragma unroll
+            for (int q = 0; q < QW; ++q)
+                if (warp / 4 * QW + q < nq) store(warp / 4 * QW + q, s_bad ? 0.f : keep[q] / s_l[warp / 4 * QW + q]);
+        }
+        for (int q = rank + warp / 4 * cs; q < nq && cs > 1; q += cs * C::NWG) {
+            const bool on = lane < cs;
+            const float mr = on ? *cluster.map_shared_rank(&s_m[q], on ? lane : 0) : -INFINITY;
+            const float lr = on ? *cluster.map_shared_rank(&s_l[q], on ? lane : 0) : 0.f;
+            const int br = on ? *cluster.map_shared_rank(&s_bad, on ? lane : 0) : 0;
+            float v[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] = r < cs && wt < HD ? *cluster.map_shared_rank(&so[q * HD + wt], r) : 0.f;
+            const float M = a8_warp_max(mr), f = mr == -INFINITY ? 0.f : a8_ex2(mr - M);
+            const float den = warp_sum(f * lr);   // a rank whose scores were all NaN: 0 x NaN
+            const bool bad = __any_sync(0xffffffffu, br);
+            float num = 0.f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) num = fmaf(__shfl_sync(0xffffffffu, f, r), v[r], num);
+            if (wt < HD) store(q, bad ? 0.f : num / den);
         }
     }
-    cluster.sync();
+    if (cs > 1) cluster.sync();   // a block's shared memory stays until its cluster has read it
 }
 
 template <typename C>
@@ -554,11 +706,10 @@ static cudaError_t launch_attn8_t(const Attn8Args &a, int sms, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     const int tiles = (a.max_rows * (a.Hq / a.Hkv) + C::QT - 1) / C::QT;
     const long long units = (long long)a.B * a.Hkv * tiles;
-    int cs = 8;
-    while (cs > 1 && units * cs > 16LL * sms) cs >>= 1;
+    const int cs = attn8_split(units, (long long)sms * C::BPS, (a.max_pages + 7) / 8);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(units * cs));
-    cfg.blockDim = dim3(A8_T);
+    cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -577,10 +728,11 @@ static cudaError_t launch_attn8_t(const Attn8Args &a, int sms, cudaStream_t s) {
 template <int HD>
 static cudaError_t launch_attn8_h(const Attn8Args &a, int sms, cudaStream_t s) {
     const int nq = a.max_rows * (a.Hq / a.Hkv);
-    if (a.q_f32) return launch_attn8_t<A8<HD, 8, 6, 6, 2>>(a, sms, s);
-    if (nq <= 8) return launch_attn8_t<A8<HD, 8, 4, 4, 3>>(a, sms, s);
-    if (nq <= 16 || a.rotate) return launch_attn8_t<A8<HD, 16, 3, 3, 2>>(a, sms, s);
-    return launch_attn8_t<A8<HD, 32, 2, 3, 2>>(a, sms, s);
+    if (a.q_f32) return nq <= 4 ? launch_attn8_t<A8<HD, 4, 4, 6, 6, 2, 3>>(a, sms, s) : launch_attn8_t<A8<HD, 8, 8, 6, 6, 2, 2>>(a, sms, s);
+    if (nq <= 4) return launch_attn8_t<A8<HD, 4, 4, 4, 4, 2, 3>>(a, sms, s);
+    if (nq <= 8) return launch_attn8_t<A8<HD, 8, 8, 4, 4, 2, 3>>(a, sms, s);
+    if (a.rotate) return launch_attn8_t<A8<HD, 32, 8, 3, 3, 1, 4>>(a, sms, s);
+    return launch_attn8_t<A8<HD, 32, 8, 2, 3, 1, 4>>(a, sms, s);
 }
 
 cudaError_t launch_attn8(const Attn8Args &a, int sms, cudaStream_t s) {

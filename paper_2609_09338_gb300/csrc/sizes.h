@@ -141,4 +141,26 @@ inline int tree_cluster(int B, double row_kb, bool greedy, const bool (&cached)[
     return pick;
 }
 
+// Blocks of a unit's cluster in the attention over the 8-bit cache (attn8.cu): the size
+// whose estimate is the least.  In tiles of 128 keys: a block takes 12 to start, merge
+// and store beside its share of the keys; units that do not all fit at once
+// (`at_once` blocks) take their mean share of the device and end with a whole one, and
+// are half as long as the longest on average.  us a call with clusters of 1, 2, 4 and 8
+// (the chosen one first): 512 units of 1024..16384 keys 2: 174 (191, 192, 259); 64 of
+// 2048..8192 4: 27 (53, 34, 37); 8 of 2048 8: 7.2 (15.2, 10.7, 8.3); 768 of up to 32
+// queries, 1024..4096 keys 1: 190 (262, 429, 886).
+inline int attn8_split(long long units, long long at_once, int tiles) {
+    int pick = 1;
+    double best = 0;
+    for (int cs = 1; cs <= 8; cs <<= 1) {
+        const double one = 12 + (double)tiles / cs;
+        const double cost = units * cs <= at_once ? one : (double)units * cs / at_once * (12 + 0.5 * tiles / cs) + one;
+        if (cs == 1 || cost < best) {
+            best = cost;
+            pick = cs;
+        }
+    }
+    return pick;
+}
+
 }  // namespace osp
