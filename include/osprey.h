@@ -253,6 +253,22 @@ int osprey_draft_step(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, int ma
                       float *draft_qx, float *draft_stats, float *draft_logits,
                       void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
 
+/* osprey_draft_step on the 8-bit cache: attention reads finished pages in 8 bits,
+ * half the bytes of the bf16 cache, which is most of a call over long contexts.
+ * The call's own rows (extend and chain) are bf16 in the tail, rounded as the
+ * bf16 cache rounds them; at the call's end the pages that the committed rows
+ * finish are rounded to 8 bits.  Verification stays lossless: it divides by the
+ * q that the tokens were drawn from.
+ *   kv: tail_pages with 16 * tail_pages >= 14 + max_new + K (CAPACITY)
+ *   workspace: osprey_draft_kv8_workspace_bytes
+ * Everything else as osprey_draft_step; B <= 4096. */
+size_t osprey_draft_kv8_workspace_bytes(const osprey_ctx *ctx, int B, int K, int max_new, int max_pages_per_seq);
+int osprey_draft_step_kv8(osprey_ctx *ctx, const osprey_kv8 *kv, int B, int K, int max_new,
+                          const int32_t *n_new, const int32_t *tokens, const void *feats,
+                          float temperature, const float *u_draft, int32_t *draft_tokens,
+                          float *draft_qx, float *draft_stats, float *draft_logits,
+                          void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
 /* osprey_draft_step with draft_logits NULL that also keeps, for every draft
  * token, the state it was drafted from, for osprey_verify_hidden:
  *   draft_hidden [B][K][d_model] float (device, 16-byte aligned): row k of

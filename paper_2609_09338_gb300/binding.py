@@ -92,6 +92,11 @@ _c_kv8_attend = _sig("osprey_kv8_attend", ctypes.c_int,
 _c_draft = _sig("osprey_draft_step", ctypes.c_int,
                 [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _f32, _vp,
                  _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp])
+_c_draft_kv8_ws = _sig("osprey_draft_kv8_workspace_bytes", _sz,
+                       [_vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int])
+_c_draft_kv8 = _sig("osprey_draft_step_kv8", ctypes.c_int,
+                    [_vp, ctypes.POINTER(osprey_kv8), ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _f32, _vp,
+                     _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp])
 _c_draft_hidden = _sig("osprey_draft_step_hidden", ctypes.c_int,
                        [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _f32,
                         _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp])
@@ -123,7 +128,8 @@ _c_launch_count = _sig("osprey_launch_count", _i64, [])
 _c_selftest_wait = _sig("osprey_selftest_wait_timeout", ctypes.c_int, [_i64, _vp, _vp])
 
 EXPORTED = ["osprey_last_error", "osprey_create", "osprey_destroy", "osprey_draft_workspace_bytes",
-            "osprey_kv_append", "osprey_kv_append_rope", "osprey_kv8_append", "osprey_kv8_attend", "osprey_draft_step", "osprey_draft_step_hidden", "osprey_draft_step_topk",
+            "osprey_kv_append", "osprey_kv_append_rope", "osprey_kv8_append", "osprey_kv8_attend",
+            "osprey_draft_kv8_workspace_bytes", "osprey_draft_step_kv8", "osprey_draft_step", "osprey_draft_step_hidden", "osprey_draft_step_topk",
             "osprey_verify_tree", "osprey_dflash_workspace_bytes",
             "osprey_dflash_step", "osprey_verify_workspace_bytes",
             "osprey_verify", "osprey_verify_static", "osprey_verify_hidden_workspace_bytes", "osprey_verify_hidden",
@@ -427,9 +433,8 @@ def osprey_kv8_attend(ctx: Ctx, kv: Kv8Cache, layer: int, n_rows: torch.Tensor, 
                          int(rotate), int(advanced), _ptr(out), _ptr(status), _stream(stream)))
 
 
-def osprey_draft_step(ctx: Ctx, kv: KvCache, n_new: torch.Tensor, tokens: torch.Tensor, feats: torch.Tensor,
-                      temperature: float, u_draft, draft_tokens: torch.Tensor, draft_qx=None, draft_stats=None,
-                      draft_logits=None, workspace: torch.Tensor = None, status: torch.Tensor = None, stream=None):
+def _draft_step(call, ctx, kv, kvs, n_new, tokens, feats, temperature, u_draft, draft_tokens, draft_qx, draft_stats,
+                draft_logits, workspace, status, stream):
     s = ctx.shape
     B, max_new = tokens.shape
     K = draft_tokens.shape[1]
@@ -449,10 +454,28 @@ def osprey_draft_step(ctx: Ctx, kv: KvCache, n_new: torch.Tensor, tokens: torch.
     _need(status, torch.int32, (1,), "status")
     if kv.page_table.shape[0] != B:
         raise ValueError("page table rows must equal the batch")
-    kvs = kv.c_struct()
-    _check(_c_draft(ctx.handle, ctypes.byref(kvs), B, K, max_new, _ptr(n_new), _ptr(tokens), _ptr(feats),
-                    float(temperature), _ptr(u_draft), _ptr(draft_tokens), _ptr(draft_qx), _ptr(draft_stats),
-                    _ptr(draft_logits), _ptr(workspace), workspace.numel(), _ptr(status), _stream(stream)))
+    _check(call(ctx.handle, ctypes.byref(kvs), B, K, max_new, _ptr(n_new), _ptr(tokens), _ptr(feats),
+                float(temperature), _ptr(u_draft), _ptr(draft_tokens), _ptr(draft_qx), _ptr(draft_stats),
+                _ptr(draft_logits), _ptr(workspace), workspace.numel(), _ptr(status), _stream(stream)))
+
+
+def osprey_draft_step(ctx: Ctx, kv: KvCache, n_new: torch.Tensor, tokens: torch.Tensor, feats: torch.Tensor,
+                      temperature: float, u_draft, draft_tokens: torch.Tensor, draft_qx=None, draft_stats=None,
+                      draft_logits=None, workspace: torch.Tensor = None, status: torch.Tensor = None, stream=None):
+    _draft_step(_c_draft, ctx, kv, kv.c_struct(), n_new, tokens, feats, temperature, u_draft, draft_tokens, draft_qx,
+                draft_stats, draft_logits, workspace, status, stream)
+
+
+def osprey_draft_kv8_workspace_bytes(ctx: Ctx, B: int, K: int, max_new: int, max_pages: int) -> int:
+    return int(_c_draft_kv8_ws(ctx.handle, B, K, max_new, max_pages))
+
+
+def osprey_draft_step_kv8(ctx: Ctx, kv: Kv8Cache, n_new: torch.Tensor, tokens: torch.Tensor, feats: torch.Tensor,
+                          temperature: float, u_draft, draft_tokens: torch.Tensor, draft_qx=None, draft_stats=None,
+                          draft_logits=None, workspace: torch.Tensor = None, status: torch.Tensor = None, stream=None):
+    """osprey_draft_step on the 8-bit cache."""
+    _draft_step(_c_draft_kv8, ctx, kv, kv.c_struct(ctx.shape), n_new, tokens, feats, temperature, u_draft, draft_tokens,
+                draft_qx, draft_stats, draft_logits, workspace, status, stream)
 
 
 def osprey_draft_step_hidden(ctx: Ctx, kv: KvCache, n_new: torch.Tensor, tokens: torch.Tensor, feats: torch.Tensor,

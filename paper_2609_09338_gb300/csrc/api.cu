@@ -543,8 +543,31 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
                            const int32_t *n_new, const int32_t *tokens, const void *feats, float temperature,
                            const float *u_draft, int32_t *draft_tokens, float *draft_qx, float *draft_stats,
                            float *draft_logits, float *draft_hidden, void *workspace, size_t workspace_bytes,
-                           int32_t *dev_status, void *stream, bool block = false, int topk = 1) {
+                           int32_t *dev_status, void *stream, bool block = false, int topk = 1,
+                           const osprey_kv8 *kv8 = nullptr) {
     g_err[0] = 0;
+    osprey_kv ring{};
+    if (ctx && kv8) {
+        // the 8-bit cache: the call's rows go to the tail, whose ring pages are a bf16 cache with a page table of
+        // its own (written by the first kernel); attention reads the finished pages in 8 bits
+        if (B == 0) return OSPREY_OK;
+        if (B < 0 || B > 4096) return fail(OSPREY_ERR_INVALID_ARG, "B must be in 0..4096");
+        const int rc = kv8_check(kv8);
+        if (rc != OSPREY_OK) return rc;
+        if (!draft_args_ok(ctx, B, K, max_new, kv8->max_pages_per_seq))
+            return fail(OSPREY_ERR_INVALID_ARG, "K and max_new in 1..64, max_pages_per_seq >= 1 required");
+        if (14 + max_new + K > 16LL * kv8->tail_pages)
+            return fail(OSPREY_ERR_CAPACITY, "the tail's ring must hold an unfinished page and the call's rows: %d positions",
+                        14 + max_new + K);
+        const size_t base = draft_layout(ctx, B, K, max_new, kv8->max_pages_per_seq, nullptr, nullptr);
+        const size_t need8 = base + 4ull * B * kv8->max_pages_per_seq;
+        if (workspace_bytes < need8)
+            return fail(OSPREY_ERR_CAPACITY, "workspace too small: %zu < %zu bytes", workspace_bytes, need8);
+        if (!workspace) return fail(OSPREY_ERR_INVALID_ARG, "null pointer");
+        ring = osprey_kv{kv8->k_tail, kv8->v_tail, (int32_t *)((char *)workspace + base), kv8->seq_len,
+                         kv8->max_pages_per_seq, B * kv8->tail_pages};
+        kv = &ring;
+    }
     if (!ctx || !kv) return fail(OSPREY_ERR_INVALID_ARG, "null context or kv");
     if (B == 0) return OSPREY_OK;
     if (!draft_args_ok(ctx, B, K, max_new, kv->max_pages_per_seq))
@@ -579,6 +602,12 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
                 kv->seq_len, n_new, tokens, kv->page_table,
                 ws.seq_valid, ws.seq_pos0, ws.seq_nnew, draft_tokens, dev_status, ws.counters, ws.n_counters,
                 block ? 1 : 0, block ? max_new : (topk > 1 ? K * topk : 0)};
+    if (kv8) {
+        pa.page_table = kv8->page_table;
+        pa.n_pages = kv8->n_pages;
+        pa.ring_table = kv->page_table;
+        pa.tail_pages = kv8->tail_pages;
+    }
     if ((e = launch_prepare(pa, s)) != cudaSuccess) return cuda_fail(e, "prepare launch");
 
     GemvArgs g{};
@@ -776,8 +805,20 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
         // several rows a sequence share their keys where that pays
         const int mt = !block && !clusters(R) && attn_rows_pays(R, D.Hq, D.Hkv, rows_per_seq, max_ctx)
                            ? attn_rows_tiles(D, rows_per_seq) : 0;
-        auto attention = [&](const AttnArgs &all) {
+        auto attention = [&](const AttnArgs &all, int l) {
             cudaError_t e2 = cudaSuccess;
+            if (kv8) {
+                Attn8Args a8{};
+                attn8_layer(ctx, kv8, l, B, a8);
+                a8.max_rows = rows_per_seq;
+                a8.map = map;
+                a8.q = all.q;
+                a8.q_f32 = 1;
+                a8.q_stride = (int64_t)D.Hq * D.hd;
+                a8.planes = all;
+                a8.status = dev_status;
+                return launch_attn8(a8, ctx->sms, s);
+            }
             for (int b0 = 0; b0 < B && e2 == cudaSuccess; b0 += grp) {   // one launch; one a group in block drafting
                 AttnArgs at = all;
                 const size_t r0 = (size_t)b0 * rows_per_seq, ha = (size_t)D.Hq * D.hd;
@@ -886,7 +927,7 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
             at.ticket = ws.attn_ticket;
             at.status = dev_status;
             if ((e = attn_probe(step * D.L + l, true)) != cudaSuccess) return cuda_fail(e, "probe record");
-            if ((e = attention(at)) != cudaSuccess) return cuda_fail(e, "attention launch");
+            if ((e = attention(at, l)) != cudaSuccess) return cuda_fail(e, "attention launch");
             if ((e = attn_probe(step * D.L + l, false)) != cudaSuccess) return cuda_fail(e, "probe record");
             // x += W_o attn;  x += W_down (silu(W_g n) * W_u n),  n = RMSNorm(x)
             const int ha = D.Hq * D.hd;
@@ -922,7 +963,7 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
             xl_ready = nxt_ready && l + 1 == D.L;
         }
         for (int l = 0; l < D.L && !tcp; ++l) {
-            if (streamed && R == 1 && ctx->fused_layer) {
+            if (streamed && R == 1 && ctx->fused_layer && !kv8) {
                 LayerArgs la{};
                 la.dim = D;
                 la.map = map;
@@ -979,7 +1020,7 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
             at.ticket = ws.attn_ticket;
             at.status = dev_status;
             if ((e = attn_probe(step * D.L + l, true)) != cudaSuccess) return cuda_fail(e, "probe record");
-            if ((e = attention(at)) != cudaSuccess) return cuda_fail(e, "attention launch");
+            if ((e = attention(at, l)) != cudaSuccess) return cuda_fail(e, "attention launch");
             if ((e = attn_probe(step * D.L + l, false)) != cudaSuccess) return cuda_fail(e, "probe record");
             if (streamed && R == 1 && ctx->fused_mlp) {
                 MlpArgs ma{};
@@ -1124,6 +1165,13 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
         if (probe && (e = probe_record(ctx->probe_end[step], s)) != cudaSuccess)
             return cuda_fail(e, "probe record");
     }
+    if (kv8) {   // pages that the committed rows finish
+        const Kv8PackArgs pk{B, D.L, D.Hkv, D.hd, kv8->max_pages_per_seq, kv8->n_pages, kv8->tail_pages, max_new,
+                             ws.seq_valid, ws.seq_pos0, ws.seq_nnew, kv8->page_table, (uint8_t *)kv8->k8,
+                             (uint8_t *)kv8->v8, kv8->k_scale, kv8->v_scale, (const uint16_t *)kv8->k_tail,
+                             (const uint16_t *)kv8->v_tail};
+        if ((e = launch_kv8_pack(pk, s)) != cudaSuccess) return cuda_fail(e, "pack launch");
+    }
     return OSPREY_OK;
 }
 
@@ -1135,6 +1183,26 @@ extern "C" int osprey_draft_step(osprey_ctx *ctx, const osprey_kv *kv, int B, in
                                  void *stream) {
     return draft_step_impl(ctx, kv, B, K, max_new, n_new, tokens, feats, temperature, u_draft, draft_tokens, draft_qx,
                            draft_stats, draft_logits, nullptr, workspace, workspace_bytes, dev_status, stream);
+}
+
+extern "C" size_t osprey_draft_kv8_workspace_bytes(const osprey_ctx *ctx, int B, int K, int max_new, int max_pages_per_seq) {
+    if (B > 4096 || !draft_args_ok(ctx, B, K, max_new, max_pages_per_seq)) return 0;
+    return draft_layout(ctx, B, K, max_new, max_pages_per_seq, nullptr, nullptr) + 4ull * B * max_pages_per_seq;
+}
+
+extern "C" int osprey_draft_step_kv8(osprey_ctx *ctx, const osprey_kv8 *kv, int B, int K, int max_new,
+                                     const int32_t *n_new, const int32_t *tokens, const void *feats,
+                                     float temperature, const float *u_draft, int32_t *draft_tokens,
+                                     float *draft_qx, float *draft_stats, float *draft_logits,
+                                     void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                     void *stream) {
+    if (!ctx || !kv) {
+        g_err[0] = 0;
+        return fail(OSPREY_ERR_INVALID_ARG, "null context or kv");
+    }
+    return draft_step_impl(ctx, nullptr, B, K, max_new, n_new, tokens, feats, temperature, u_draft, draft_tokens, draft_qx,
+                           draft_stats, draft_logits, nullptr, workspace, workspace_bytes, dev_status, stream, false, 1,
+                           kv);
 }
 
 extern "C" int osprey_draft_step_hidden(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, int max_new,

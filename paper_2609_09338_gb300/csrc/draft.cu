@@ -932,6 +932,9 @@ __global__ void __launch_bounds__(128) prepare_kernel(const PrepArgs a) {
         if (ok) a.seq_len[b] = L0 + (a.commit > 0 ? a.commit : nn);
         else set_status(a.status, code);
     }
+    if (a.ring_table && ok)
+        for (int pg = L0 / 16 + threadIdx.x; pg <= (L0 + nn + a.K - 2) / 16; pg += blockDim.x)
+            a.ring_table[(size_t)b * a.max_pages + pg] = b * a.tail_pages + pg % a.tail_pages;
     const int n_out = a.n_out > 0 ? a.n_out : a.K;
     if (!ok)
         for (int k = threadIdx.x; k < n_out; k += blockDim.x) a.draft_tokens[(size_t)b * n_out + k] = -1;

@@ -160,6 +160,10 @@ struct PrepArgs {
     int n_counters;
     int commit;    // rows committed per sequence (0: all n_new rows)
     int n_out;     // draft tokens per sequence set to -1 for a skipped sequence (0: K)
+    // a call on the 8-bit cache: the page table of its tail, ring pages b tail_pages + p % tail_pages, written here
+    // for the pages of the call's rows
+    int32_t *ring_table;
+    int tail_pages;
 };
 
 enum GemvMode { G_FEAT = 0, G_QKV = 1, G_OPROJ = 2, G_GATEUP = 3, G_DOWN = 4, G_LM = 5 };

@@ -68,6 +68,38 @@ class DraftSession:
                                     self.status, stream)
 
 
+class Kv8DraftSession(DraftSession):
+    """A drafter on the 8-bit K/V cache: codes of finished pages, a bf16 ring for the rows of a call."""
+
+    def __init__(self, shape: DrafterShape, weights_np: dict, page_table: np.ndarray, n_pages: int, K: int,
+                 max_new: int = 1, device: str = "cuda"):
+        self.shape, self.K, self.max_new, self.device = shape, K, max_new, device
+        self.weights = ob.upload_weights(weights_np, device)
+        self.ctx = ob.osprey_create(shape, self.weights)
+        # the ring holds an unfinished page and the call's extend and chain rows
+        self.kv = ob.alloc_kv8(shape, page_table, n_pages, (14 + max_new + K + 15) // 16, device)
+        self.B = page_table.shape[0]
+        nbytes = ob.osprey_draft_kv8_workspace_bytes(self.ctx, self.B, K, max_new, self.kv.max_pages)
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def append(self, n_rows: np.ndarray, k_rows: np.ndarray, v_rows: np.ndarray):
+        ob.osprey_kv8_append(self.ctx, self.kv, torch.from_numpy(np.asarray(n_rows, np.int32)).to(self.device),
+                             ob.to_device_bf16(k_rows, self.device), ob.to_device_bf16(v_rows, self.device),
+                             self.status, rotate=False)
+
+    def draft(self, n_new, tokens, feats, temperature: float, u_draft, out: dict, stream=None):
+        ob.osprey_draft_step_kv8(self.ctx, self.kv, n_new, tokens, feats, temperature, u_draft, out["draft_tokens"],
+                                 out["draft_qx"], out["draft_stats"], out["draft_logits"], self.workspace,
+                                 self.status, stream)
+
+    def draft_tree(self, *args, **kw):
+        raise NotImplementedError("tree drafting runs on the bf16 cache")
+
+    def draft_hidden(self, *args, **kw):
+        raise NotImplementedError("drafting with kept states runs on the bf16 cache")
+
+
 class DflashSession(DraftSession):
     """A drafter that proposes blocks (EAGLE-style DFlash): each call is one
     forward over the anchor and block - 1 mask positions of every sequence."""
