@@ -11,34 +11,33 @@ namespace osp {
 
 constexpr int KR_THREADS = 256;
 constexpr int KR_WARPS = KR_THREADS / 32;
-constexpr int KR_BLOCKS_PER_SM = 3;
 
-// Exclusive prefix of one int64 per thread over the block; *total: the sum.
-__device__ __forceinline__ int64_t kr_scan(int64_t v, int64_t *sh, int64_t *total) {
+// Exclusive prefixes of two int64 a thread over the block, and their sums.
+__device__ __forceinline__ void kr_scan(int64_t &x, int64_t &y, int64_t (*sh)[2], int64_t &sum_x, int64_t &sum_y) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    int64_t inc = v;
+    int64_t ix = x, iy = y;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t n = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += n;
+        const int64_t nx = __shfl_up_sync(0xffffffffu, ix, o), ny = __shfl_up_sync(0xffffffffu, iy, o);
+        if (lane >= o) ix += nx, iy += ny;
     }
-    if (lane == 31) sh[w] = inc;
+    if (lane == 31) sh[w][0] = ix, sh[w][1] = iy;
     __syncthreads();
-    int64_t before = 0, tot = 0;
+    x = ix - x;
+    y = iy - y;
+    sum_x = sum_y = 0;
 #pragma unroll
     for (int k = 0; k < KR_WARPS; ++k) {
-        if (k < w) before += sh[k];
-        tot += sh[k];
+        if (k < w) x += sh[k][0], y += sh[k][1];
+        sum_x += sh[k][0];
+        sum_y += sh[k][1];
     }
-    __syncthreads();
-    *total = tot;
-    return before + inc - v;
 }
 
 // Pages that n rows after L0 touch.
 __device__ __forceinline__ int kr_pages(int L0, int n) { return n > 0 ? (L0 + n - 1) / 16 - L0 / 16 + 1 : 0; }
 
-// One warp's block of one page and head while it is in registers, as bf16 pairs.
+// One warp's block of one page and head (K or V) in registers, 16 rows x HD as bf16 pairs.
 // K: the lane's items are (row, 8 dims, the 8 dims hd / 2 further), the halves that the
 // rotation mixes.  V: the lane holds HD / 32 dims of all 16 rows, so that it can write
 // a dim's 16 slots at once.
@@ -47,49 +46,55 @@ struct KvBlock {
     static constexpr int C = HD / 16;       // K: 8-dim chunks of half a row
     static constexpr int RPI = 32 / C;      // K: rows an iteration
     static constexpr int NK = 16 / RPI;     // K: iterations
-    static constexpr int NV = HD / 64;      // V: 32-bit words of a lane's dims
-    uint4 lo[NK], hi[NK];
-    uint32_t v[16][NV];
+    static constexpr int NV = HD / 64;      // V: 32-bit words of a lane's dims of one row
+    static constexpr int W = 16 * NV;       // words of a lane's share, of K too (8 an iteration: low, then high half)
 };
 
-// codes of the block and its scale, from bf16 values
+// The block's scale: its exponent (0 for a block with an infinity or a NaN, *bad)
+template <int W>
+__device__ __forceinline__ int kv8_scale(const uint32_t (&x)[W], float *scale, bool &bad) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) m = __vmaxu2(m, x[i] & 0x7fff7fffu);
+    m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+    bad = m >= 0x7f80u;
+    const int e = bad ? 0 : kv8_exp(m);
+    if ((threadIdx.x & 31) == 0) *scale = bad ? __uint_as_float(0x7fffffffu) : kv8_pow2(e);
+    return e;
+}
+
+// codes of a K block and its scale, from bf16 values
 template <int HD>
-__device__ __forceinline__ void kv8_quantise(const KvBlock<HD> &x, uint8_t *k8, uint8_t *v8, float *ks, float *vs) {
+__device__ __forceinline__ void kv8_quantise_k(const uint32_t (&x)[KvBlock<HD>::W], uint8_t *dst, float *scale) {
     using B = KvBlock<HD>;
-    const int lane = threadIdx.x & 31;
-    auto mag2 = [](uint32_t w) { return max(w & 0x7fffu, (w >> 16) & 0x7fffu); };
-    uint32_t km = 0, vm = 0;
-#pragma unroll
-    for (int i = 0; i < B::NK; ++i)
-        km = max(km, max(max(max(mag2(x.lo[i].x), mag2(x.lo[i].y)), max(mag2(x.lo[i].z), mag2(x.lo[i].w))),
-                         max(max(mag2(x.hi[i].x), mag2(x.hi[i].y)), max(mag2(x.hi[i].z), mag2(x.hi[i].w)))));
-#pragma unroll
-    for (int t = 0; t < 16; ++t)
-#pragma unroll
-        for (int j = 0; j < B::NV; ++j) vm = max(vm, mag2(x.v[t][j]));
-    km = __reduce_max_sync(0xffffffffu, km);
-    vm = __reduce_max_sync(0xffffffffu, vm);
-    const bool kbad = km >= 0x7f80u, vbad = vm >= 0x7f80u;   // an infinity or a NaN
-    const int ke = kv8_exp(km), ve = kv8_exp(vm);
-    if (lane == 0) {
-        *ks = kbad ? __uint_as_float(0x7fffffffu) : kv8_pow2(ke);
-        *vs = vbad ? __uint_as_float(0x7fffffffu) : kv8_pow2(ve);
-    }
-    const float ki = kv8_pow2(kbad ? 0 : -ke), vi = kv8_pow2(vbad ? 0 : -ve);
-    auto code8 = [&](const uint4 &w) {
-        uint2 r;
-        r.x = e4m3x2(bf_lo(w.x) * ki, bf_hi(w.x) * ki) | e4m3x2(bf_lo(w.y) * ki, bf_hi(w.y) * ki) << 16;
-        r.y = e4m3x2(bf_lo(w.z) * ki, bf_hi(w.z) * ki) | e4m3x2(bf_lo(w.w) * ki, bf_hi(w.w) * ki) << 16;
-        return kbad ? make_uint2(0, 0) : r;
-    };
-    const int c = lane % B::C;
+    const int lane = threadIdx.x & 31, c = lane % B::C;
+    bool bad;
+    const float inv = kv8_pow2(-kv8_scale(x, scale, bad));
 #pragma unroll
     for (int i = 0; i < B::NK; ++i) {
         const int r = lane / B::C + i * B::RPI;
-        auto at = [&](int d) { return ((r >> 3) * (HD / 16) + (d >> 4)) * 128 + (r & 7) * 16 + (d & 15); };
-        *(uint2 *)(k8 + at(c * 8)) = code8(x.lo[i]);
-        *(uint2 *)(k8 + at(HD / 2 + c * 8)) = code8(x.hi[i]);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            uint32_t w[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t u = x[8 * i + 4 * half + 2 * j], v = x[8 * i + 4 * half + 2 * j + 1];
+                w[j] = e4m3x2(bf_lo(u) * inv, bf_hi(u) * inv) | e4m3x2(bf_lo(v) * inv, bf_hi(v) * inv) << 16;
+            }
+            const int d = half * (HD / 2) + c * 8;
+            *(uint2 *)(dst + ((r >> 3) * (HD / 16) + (d >> 4)) * 128 + (r & 7) * 16 + (d & 15)) =
+                bad ? make_uint2(0, 0) : make_uint2(w[0], w[1]);
+        }
     }
+}
+
+// ... of a V block
+template <int HD>
+__device__ __forceinline__ void kv8_quantise_v(const uint32_t (&x)[KvBlock<HD>::W], uint8_t *dst, float *scale) {
+    using B = KvBlock<HD>;
+    const int lane = threadIdx.x & 31;
+    bool bad;
+    const float inv = kv8_pow2(-kv8_scale(x, scale, bad));
 #pragma unroll
     for (int j = 0; j < B::NV; ++j)
 #pragma unroll
@@ -97,52 +102,70 @@ __device__ __forceinline__ void kv8_quantise(const KvBlock<HD> &x, uint8_t *k8, 
             uint32_t w[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                auto val = [&](int t) { return (h ? bf_hi(x.v[t][j]) : bf_lo(x.v[t][j])) * vi; };
+                auto val = [&](int t) { return (h ? bf_hi(x[t * B::NV + j]) : bf_lo(x[t * B::NV + j])) * inv; };
                 w[g] = e4m3x2(val(4 * g), val(4 * g + 1)) | e4m3x2(val(4 * g + 2), val(4 * g + 3)) << 16;
             }
-            const int d = lane * (HD / 32) + 2 * j + h;
-            *(uint4 *)(v8 + d * 16) = vbad ? make_uint4(0, 0, 0, 0) : make_uint4(w[0], w[1], w[2], w[3]);
+            *(uint4 *)(dst + (lane * (HD / 32) + 2 * j + h) * 16) =
+                bad ? make_uint4(0, 0, 0, 0) : make_uint4(w[0], w[1], w[2], w[3]);
         }
 }
 
-// rows r0 .. r1 - 1 of the block from the page of bf16 rows (16 x HD) at kp and vp
-template <int HD>
-__device__ __forceinline__ void kv8_from_tail(KvBlock<HD> &x, const uint16_t *kp, const uint16_t *vp, int r0, int r1) {
+// rows r0 .. r1 - 1 of a block from (or to) a page of bf16 rows (16 x HD)
+template <int HD, bool STORE, typename T>
+__device__ __forceinline__ void kv8_rows_k(uint32_t (&x)[KvBlock<HD>::W], T *page, int r0, int r1) {
     using B = KvBlock<HD>;
     const int lane = threadIdx.x & 31, c = lane % B::C;
 #pragma unroll
     for (int i = 0; i < B::NK; ++i) {
         const int r = lane / B::C + i * B::RPI;
         if (r < r0 || r >= r1) continue;
-        x.lo[i] = *(const uint4 *)(kp + r * HD + c * 8);
-        x.hi[i] = *(const uint4 *)(kp + r * HD + HD / 2 + c * 8);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            auto *at = page + r * HD + half * (HD / 2) + c * 8;
+            uint32_t *w = x + 8 * i + 4 * half;
+            if constexpr (STORE) {
+                *(uint4 *)at = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                const uint4 v = *(const uint4 *)at;
+                w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+            }
+        }
     }
+}
+template <int HD, bool STORE, typename T>
+__device__ __forceinline__ void kv8_rows_v(uint32_t (&x)[KvBlock<HD>::W], T *page, int r0, int r1) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int t = 0; t < 16; ++t) {
         if (t < r0 || t >= r1) continue;
-        const uint16_t *p = vp + t * HD + lane * (HD / 32);
+        auto *at = page + t * HD + lane * (HD / 32);
         if constexpr (HD == 128) {
-            const uint2 w = *(const uint2 *)p;
-            x.v[t][0] = w.x;
-            x.v[t][1] = w.y;
+            if constexpr (STORE) {
+                *(uint2 *)at = make_uint2(x[2 * t], x[2 * t + 1]);
+            } else {
+                const uint2 w = *(const uint2 *)at;
+                x[2 * t] = w.x;
+                x[2 * t + 1] = w.y;
+            }
         } else {
-            x.v[t][0] = *(const uint32_t *)p;
+            if constexpr (STORE) *(uint32_t *)at = x[t];
+            else x[t] = *(const uint32_t *)at;
         }
     }
 }
 
 // Bound by memory for prompts, by latency for a decode step.  A unit is one page of
 // one sequence, for all layers and heads: the angles of its new positions are made
-// once (fixed-point turns, then sincospif) and shared by its warps, which take one
-// layer and head at a time through registers: rows are read once, rotated, and
+// once (fixed-point turns, then sincospif) and shared by its warps, which take K or V
+// of one layer and head at a time through registers: rows are read once, rotated, and
 // written in bf16 (to the page, or to the tail) or, where the page is finished,
-// as codes.  Units are found by a scan over the batch that each block keeps in
-// registers.
+// as codes.  A warp's first rows are on their way while the angles are made.  Units
+// are found by a scan over the batch that each block keeps in registers.
 template <int HD, bool EIGHT, bool RF32>
-__global__ void __launch_bounds__(KR_THREADS, 2) kv_rope_kernel(const KvRopeArgs a) {
-    __shared__ int64_t sh[KR_WARPS];
-    __shared__ float2 cs[16][HD / 2];
-    __shared__ int s_b, s_page;
+__global__ void __launch_bounds__(KR_THREADS, RF32 ? 2 : 3) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
+    __shared__ int64_t sh[KR_WARPS][2];
+    __shared__ __align__(16) float2 cs[16][HD / 2];   // pairs of dims e, e + 1 of chunk c at (e / 2) C + c: lanes side by side
+    __shared__ int s_b, s_page, s_L0, s_n;
     __shared__ int64_t s_row;
     using Blk = KvBlock<HD>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -157,7 +180,9 @@ __global__ void __launch_bounds__(KR_THREADS, 2) kv_rope_kernel(const KvRopeArgs
         // a sequence that does not fit has one unit, which reports it
         pages += n > 0 && (L0 < 0 || (int64_t)L0 + n > (int64_t)a.max_pages * 16) ? 1 : kr_pages(L0, n);
     }
-    const int64_t row0 = kr_scan(rows, sh, &total), unit0 = kr_scan(pages, sh, &units);
+    const int64_t my_pages = pages;
+    int64_t row0 = rows, unit0 = pages;
+    kr_scan(row0, unit0, sh, total, units);
     if (__syncthreads_or(neg) || total != a.total_rows) {
         if (threadIdx.x == 0) set_status(a.status, OSPREY_ERR_INVALID_ARG);
         return;
@@ -165,8 +190,10 @@ __global__ void __launch_bounds__(KR_THREADS, 2) kv_rope_kernel(const KvRopeArgs
     pdl_trigger();
     int last_b = -1;
     bool last_ok = false;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        if (u >= unit0 && u < unit0 + pages) {
+    // a contiguous range of the units: a sequence's pages are checked once a block
+    const int64_t u0 = units * blockIdx.x / gridDim.x, u1 = units * (blockIdx.x + 1) / gridDim.x;
+    for (int64_t u = u0; u < u1; ++u) {
+        if (u >= unit0 && u < unit0 + my_pages) {
             int64_t at = unit0, r = row0;
             for (int b = b0; b < b1; ++b) {
                 const int n = a.n_rows[b], L0 = a.seq_len[b];
@@ -175,6 +202,8 @@ __global__ void __launch_bounds__(KR_THREADS, 2) kv_rope_kernel(const KvRopeArgs
                     s_b = b;
                     s_page = (int)(u - at);
                     s_row = r;
+                    s_L0 = L0;
+                    s_n = n;
                     break;
                 }
                 at += np;
@@ -184,7 +213,7 @@ __global__ void __launch_bounds__(KR_THREADS, 2) kv_rope_kernel(const KvRopeArgs
         __syncthreads();
         const int b = s_b;
         const int64_t row = s_row;
-        const int L0 = a.seq_len[b], n = a.n_rows[b], end = L0 + n;
+        const int L0 = s_L0, n = s_n, end = L0 + n;
         const int32_t *tab = a.page_table + (size_t)b * a.max_pages;
         if (b != last_b) {   // every page that the rows touch has to be good: the sequence is left as it is otherwise
             bool bad = L0 < 0 || (int64_t)L0 + n > (int64_t)a.max_pages * 16;
@@ -199,120 +228,121 @@ __global__ void __launch_bounds__(KR_THREADS, 2) kv_rope_kernel(const KvRopeArgs
             __syncthreads();   // s_b is read by all before the next unit writes it
             continue;
         }
-        const int p0 = L0 / 16, plast = (end - 1) / 16, TP = EIGHT ? a.tail_pages : 1;
-        // One page.  The ring page of p0 holds older rows that its block needs; the new
-        // page that falls on the same ring page is written by p0's unit after that.
-        auto page_rows = [&](int p, bool codes, bool tail) {
+        const int p0 = L0 / 16, plast = (end - 1) / 16, TP = EIGHT ? a.tail_pages : 1, mine = p0 + s_page;
+        // The ring page of p0 holds older rows that its block needs; the last new page that
+        // falls on the same ring page (`clash`) is written by p0's unit, after that.
+        const int clash = EIGHT && L0 % 16 ? plast - (plast - p0) % TP : p0;
+        for (int pass = 0; pass < 2; ++pass) {
+            if (pass == 1 && !(EIGHT && mine == p0 && clash != p0)) break;
+            const int p = pass == 0 ? mine : clash;
+            const bool tail = pass == 1 || (p > plast - TP && (p == p0 || p != clash));
             const int t0 = max(0, L0 - p * 16), t1 = min(16, end - p * 16);
-            if (a.rotate)
-                for (int i = threadIdx.x; i < (t1 - t0) * (HD / 2); i += KR_THREADS) {
-                    const int t = t0 + i / (HD / 2), d = i % (HD / 2);
-                    rope_cs_fix(a.freq[d], p * 16 + t, cs[t][d].x, cs[t][d].y);
-                }
-            __syncthreads();
-            const bool full = EIGHT && codes && t1 == 16;
-            if (EIGHT && !full && !tail) return;
-            const int page = tab[p];
-            for (int it = warp; it < a.layers * a.Hkv; it += KR_WARPS) {
-                const int l = it / a.Hkv, h = it - l * a.Hkv, layer = a.layer0 + l;
-                const size_t blk = ((size_t)layer * a.n_pages + page) * a.Hkv + h;
-                uint16_t *kd, *vd;   // this page's bf16 rows
-                if (EIGHT) {
-                    const size_t t = (((size_t)layer * a.B + b) * TP + p % TP) * a.Hkv + h;
-                    kd = a.k_tail + t * 16 * HD;
-                    vd = a.v_tail + t * 16 * HD;
-                } else {
-                    kd = a.k_pages + blk * 16 * HD;
-                    vd = a.v_pages + blk * 16 * HD;
-                }
-                Blk x;
+            const bool full = EIGHT && pass == 0 && t1 == 16, work = !EIGHT || full || tail;
+            const int page = tab[p], items = work ? 2 * a.layers * a.Hkv : 0;
+            __align__(16) uint32_t x[Blk::W], f[RF32 ? 2 * Blk::W : 1];   // the lane's share of the block; float32 rows as they come
+            auto fetch = [&](int it) {
+                const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
                 const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;   // row of slot 0
-                const int c = lane % Blk::C;
+                const int64_t at0 = first * a.row_stride + h * HD;
 #pragma unroll
-                for (int i = 0; i < Blk::NK; ++i) {
-                    const int r = lane / Blk::C + i * Blk::RPI;
-                    x.lo[i] = x.hi[i] = make_uint4(0, 0, 0, 0);
-                    if (r < t0 || r >= t1) continue;
-                    const int64_t at = (first + r) * a.row_stride + h * HD + c * 8;
-                    float f[8], g[8];
+                for (int i = 0; i < Blk::W; ++i) x[i] = 0;
+                if ((it & 1) == 0) {
                     if constexpr (RF32) {
-                        const float *src = (const float *)a.k_rows + at;
-                        *(uint4 *)f = ld_stream(src);
-                        *(uint4 *)(f + 4) = ld_stream(src + 4);
-                        *(uint4 *)g = ld_stream(src + HD / 2);
-                        *(uint4 *)(g + 4) = ld_stream(src + HD / 2 + 4);
-                    } else {
-                        const uint16_t *src = (const uint16_t *)a.k_rows + at;
-                        unpack8(ld_stream(src), f);
-                        unpack8(ld_stream(src + HD / 2), g);
-                    }
-                    if (a.rotate)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float2 w = cs[r][c * 8 + e];
-                            const float y = f[e] * w.x - g[e] * w.y;
-                            g[e] = g[e] * w.x + f[e] * w.y;
-                            f[e] = y;
-                        }
-                    x.lo[i] = make_uint4(kv8_bf2(f[0], f[1]), kv8_bf2(f[2], f[3]), kv8_bf2(f[4], f[5]), kv8_bf2(f[6], f[7]));
-                    x.hi[i] = make_uint4(kv8_bf2(g[0], g[1]), kv8_bf2(g[2], g[3]), kv8_bf2(g[4], g[5]), kv8_bf2(g[6], g[7]));
-                }
+                        for (int i = 0; i < Blk::NK; ++i) {
+                            const int r = lane / Blk::C + i * Blk::RPI;
+                            if (r < t0 || r >= t1) continue;
+                            const uint4 *src = (const uint4 *)((const float *)a.k_rows + at0 + r * a.row_stride + lane % Blk::C * 8);
 #pragma unroll
-                for (int t = 0; t < 16; ++t) {
-#pragma unroll
-                    for (int j = 0; j < Blk::NV; ++j) x.v[t][j] = 0;
-                    if (t < t0 || t >= t1) continue;
-                    const int64_t at = (first + t) * a.row_stride + h * HD + lane * (HD / 32);
-                    if constexpr (RF32) {
-                        const float *src = (const float *)a.v_rows + at;
-                        if constexpr (HD == 128) {
-                            const float4 f = *(const float4 *)src;
-                            x.v[t][0] = kv8_bf2(f.x, f.y);
-                            x.v[t][1] = kv8_bf2(f.z, f.w);
-                        } else {
-                            const float2 f = *(const float2 *)src;
-                            x.v[t][0] = kv8_bf2(f.x, f.y);
+                            for (int j = 0; j < 4; ++j) *(uint4 *)(f + 16 * i + 4 * j) = __ldg(src + (j >> 1) * (HD / 8) + (j & 1));
                         }
                     } else {
-                        const uint16_t *src = (const uint16_t *)a.v_rows + at;
-                        if constexpr (HD == 128) {
-                            const uint2 w = *(const uint2 *)src;
-                            x.v[t][0] = w.x;
-                            x.v[t][1] = w.y;
-                        } else {
-                            x.v[t][0] = *(const uint32_t *)src;
+#pragma unroll
+                        for (int i = 0; i < Blk::NK; ++i) {
+                            const int r = lane / Blk::C + i * Blk::RPI;
+                            if (r < t0 || r >= t1) continue;
+                            const uint16_t *src = (const uint16_t *)a.k_rows + at0 + r * a.row_stride + lane % Blk::C * 8;
+                            *(uint4 *)(x + 8 * i) = ld_stream(src);
+                            *(uint4 *)(x + 8 * i + 4) = ld_stream(src + HD / 2);
                         }
                     }
-                }
-                if (!EIGHT || tail) {
-#pragma unroll
-                    for (int i = 0; i < Blk::NK; ++i) {
-                        const int r = lane / Blk::C + i * Blk::RPI;
-                        if (r < t0 || r >= t1) continue;
-                        *(uint4 *)(kd + r * HD + c * 8) = x.lo[i];
-                        *(uint4 *)(kd + r * HD + HD / 2 + c * 8) = x.hi[i];
-                    }
+                } else {
 #pragma unroll
                     for (int t = 0; t < 16; ++t) {
                         if (t < t0 || t >= t1) continue;
-                        uint16_t *dst = vd + t * HD + lane * (HD / 32);
-                        if constexpr (HD == 128) *(uint2 *)dst = make_uint2(x.v[t][0], x.v[t][1]);
-                        else *(uint32_t *)dst = x.v[t][0];
+                        const int64_t at = at0 + t * a.row_stride + lane * (HD / 32);
+                        if constexpr (RF32) {
+                            const float *src = (const float *)a.v_rows + at;
+                            if constexpr (HD == 128) *(uint4 *)(f + 4 * t) = __ldg((const uint4 *)src);
+                            else *(uint2 *)(f + 2 * t) = __ldg((const uint2 *)src);
+                        } else {
+                            const uint16_t *src = (const uint16_t *)a.v_rows + at;
+                            if constexpr (HD == 128) *(uint2 *)(x + 2 * t) = __ldg((const uint2 *)src);
+                            else x[t] = __ldg((const uint32_t *)src);
+                        }
                     }
                 }
-                if (full) {
-                    kv8_from_tail<HD>(x, kd, vd, 0, t0);   // older rows (t0 > 0: p is p0, its own ring page)
-                    kv8_quantise<HD>(x, a.k8 + blk * 16 * HD, a.v8 + blk * 16 * HD, a.k_scale + blk, a.v_scale + blk);
+            };
+            if (pass == 1) __syncthreads();   // p0's older rows are read, and so are its angles
+            if (warp < items) fetch(warp);
+            if (a.rotate && work)
+                for (int i = threadIdx.x; i < (t1 - t0) * (HD / 2); i += KR_THREADS) {
+                    const int t = t0 + i / (HD / 2), d = i % (HD / 2);
+                    float2 &w = cs[t][((d >> 1 & 3) * Blk::C + (d >> 3)) * 2 + (d & 1)];
+                    rope_cs_fix(a.freq[d], p * 16 + t, w.x, w.y);
+                }
+            __syncthreads();
+            for (int it = warp; it < items; it += KR_WARPS) {
+                const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv, layer = a.layer0 + l;
+                const size_t blk = ((size_t)layer * a.n_pages + page) * a.Hkv + h;
+                // this page's bf16 rows: the tail's, or the page's own
+                const size_t at = (EIGHT ? (((size_t)layer * a.B + b) * TP + p % TP) * a.Hkv + h : blk) * 16 * HD;
+                if (it != warp) fetch(it);
+                if ((it & 1) == 0) {
+#pragma unroll
+                    for (int i = 0; i < Blk::NK; ++i) {
+                        const int r = lane / Blk::C + i * Blk::RPI;
+                        if (r < t0 || r >= t1 || (!RF32 && !a.rotate)) continue;
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {   // pairs of dims and their partners
+                            float u[2], v[2];
+                            uint32_t &lo = x[8 * i + e / 2], &hi = x[8 * i + 4 + e / 2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                u[k] = RF32 ? __uint_as_float(f[(RF32 ? 16 * i + e + k : 0)]) : k ? bf_hi(lo) : bf_lo(lo);
+                                v[k] = RF32 ? __uint_as_float(f[(RF32 ? 16 * i + 8 + e + k : 0)]) : k ? bf_hi(hi) : bf_lo(hi);
+                            }
+                            if (a.rotate) {
+                                const float4 w = *(const float4 *)&cs[r][(e / 2 * Blk::C + lane % Blk::C) * 2];
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const float c = k ? w.z : w.x, s = k ? w.w : w.y, y = u[k] * c - v[k] * s;
+                                    v[k] = v[k] * c + u[k] * s;
+                                    u[k] = y;
+                                }
+                            }
+                            lo = kv8_bf2(u[0], u[1]);
+                            hi = kv8_bf2(v[0], v[1]);
+                        }
+                    }
+                    uint16_t *bf = (EIGHT ? a.k_tail : a.k_pages) + at;
+                    if (!EIGHT || tail) kv8_rows_k<HD, true>(x, bf, t0, t1);
+                    if (full) {
+                        kv8_rows_k<HD, false>(x, bf, 0, t0);   // older rows (t0 > 0: p is p0, its own ring page)
+                        kv8_quantise_k<HD>(x, a.k8 + blk * 16 * HD, a.k_scale + blk);
+                    }
+                } else {
+                    if constexpr (RF32)
+#pragma unroll
+                        for (int i = 0; i < Blk::W; ++i) x[i] = kv8_bf2(__uint_as_float(f[2 * i]), __uint_as_float(f[2 * i + 1]));
+                    uint16_t *bf = (EIGHT ? a.v_tail : a.v_pages) + at;
+                    if (!EIGHT || tail) kv8_rows_v<HD, true>(x, bf, t0, t1);
+                    if (full) {
+                        kv8_rows_v<HD, false>(x, bf, 0, t0);
+                        kv8_quantise_v<HD>(x, a.v8 + blk * 16 * HD, a.v_scale + blk);
+                    }
                 }
             }
-        };
-        const int p = p0 + s_page;
-        // the last page on p0's ring page, where that holds older rows
-        const int clash = EIGHT && L0 % 16 ? plast - (plast - p0) % TP : p0;
-        page_rows(p, true, p > plast - TP && (p == p0 || p != clash));
-        if (EIGHT && p == p0 && clash != p0) {
-            __syncthreads();   // p0's older rows are read, and so are its angles
-            page_rows(clash, false, true);
         }
         __syncthreads();   // cs and s_b are read
     }
@@ -326,7 +356,7 @@ static cudaError_t launch_kv_rope_t(const KvRopeArgs &a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     // units: n rows touch at most n / 16 + 2 pages, and no more pages than rows
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.total_rows, a.total_rows / 16 + 2LL * a.B));
-    const int64_t cap = (int64_t)KR_BLOCKS_PER_SM * sms;
+    const int64_t cap = (RF32 ? 2LL : 3LL) * sms;   // as many as are resident
     kv_rope_kernel<HD, EIGHT, RF32><<<(unsigned)std::min(most, cap), KR_THREADS, 0, s>>>(a);
     count_launch();
     return cudaGetLastError();
@@ -354,8 +384,8 @@ cudaError_t launch_kv_rope(const KvRopeArgs &a, bool eight, bool advance, cudaSt
     return launch_kv_advance(v, true, s);
 }
 
-// Finished pages of a draft call's committed rows, from the tail: one warp a layer and
-// head, one block a page.
+// Finished pages of a draft call's committed rows, from the tail: one warp K or V of a
+// layer and head, one block a page.
 template <int HD>
 __global__ void __launch_bounds__(KR_THREADS) kv8_pack_kernel(const Kv8PackArgs a) {
     const int b = blockIdx.y, warp = threadIdx.x >> 5;
@@ -363,13 +393,18 @@ __global__ void __launch_bounds__(KR_THREADS) kv8_pack_kernel(const Kv8PackArgs 
     const int p = a.pos0[b] / 16 + blockIdx.x;
     if ((p + 1) * 16 > a.pos0[b] + a.nnew[b]) return;
     const int page = a.page_table[(size_t)b * a.max_pages + p];   // in range: the call's first kernel has checked it
-    for (int it = warp; it < a.L * a.Hkv; it += KR_WARPS) {
-        const int l = it / a.Hkv, h = it - l * a.Hkv;
+    for (int it = warp; it < 2 * a.L * a.Hkv; it += KR_WARPS) {
+        const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
         const size_t t = ((((size_t)l * a.B + b) * a.tail_pages + p % a.tail_pages) * a.Hkv + h) * 16 * HD;
         const size_t blk = ((size_t)l * a.n_pages + page) * a.Hkv + h;
-        KvBlock<HD> x;
-        kv8_from_tail<HD>(x, a.k_tail + t, a.v_tail + t, 0, 16);
-        kv8_quantise<HD>(x, a.k8 + blk * 16 * HD, a.v8 + blk * 16 * HD, a.k_scale + blk, a.v_scale + blk);
+        __align__(16) uint32_t x[KvBlock<HD>::W];
+        if ((it & 1) == 0) {
+            kv8_rows_k<HD, false>(x, a.k_tail + t, 0, 16);
+            kv8_quantise_k<HD>(x, a.k8 + blk * 16 * HD, a.k_scale + blk);
+        } else {
+            kv8_rows_v<HD, false>(x, a.v_tail + t, 0, 16);
+            kv8_quantise_v<HD>(x, a.v8 + blk * 16 * HD, a.v_scale + blk);
+        }
     }
 }
 
