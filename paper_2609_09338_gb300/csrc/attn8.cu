@@ -36,7 +36,7 @@ namespace osp {
 namespace cg = cooperative_groups;
 
 constexpr int A8_CH = 32;            // tail keys of a step
-constexpr int A8_PCH = 144;          // bytes between the weights' core matrices: 128 and 4 banks, so that a warp's two do not meet
+constexpr int A8_PG = 2048;          // bytes of 16 weight columns of a tile
 constexpr float A8_LO = -40.f;       // smallest log2 of a V scale that moves the reference
 constexpr float A8_OVER = 4.f;       // a weight is at most 2^A8_OVER, times A8_UP an e4m3 number
 constexpr float A8_UP = 16.f;
@@ -55,20 +55,24 @@ struct A8 {
     static constexpr int USED = NSB * SC + OC;
     static constexpr int COLS = USED <= 32 ? 32 : USED <= 64 ? 64 : USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
     static constexpr int QB = SC * HD;                    // bytes of q's planes
-    static constexpr int PW = 8 * A8_PCH * (OC / 8);         // bytes of the weights' planes
+    static constexpr int PW = A8_PG * (OC / 16);          // bytes of the weights' planes
     static constexpr int PB = PW > QT * HD * 4 ? PW : QT * HD * 4;   // their place, q's for the tail
     static constexpr int SMEM = 2 * NS * TB + QB + PB + QT * A8_CH * 4;
-    static_assert(COLS <= TM && QB + PB >= KB && QT % QW == 0, "operands");
+    static_assert((QW == 4 || QW == 8) && COLS <= TM && QB + PB >= KB && QT % QW == 0, "operands");
     static_assert(QT * HD * 4 <= NS * TB, "the merge's outputs take the K slots");
 };
 
-// Shared-memory matrix descriptor of a K-major operand without swizzle: core matrices
-// of 8 rows x 16 bytes, lbo bytes apart along the reduction, sbo along the rows.
+// Shared-memory matrix descriptor of an operand without swizzle.  K-major: core matrices
+// of 8 rows x 16 bytes, lbo bytes apart along the reduction, sbo along the rows.  The
+// weights lie the other way round, 8 keys x 16 columns (lbo still along the reduction), so
+// that a thread, which is a key, writes its queries' weights side by side.
 __device__ __forceinline__ uint64_t a8_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46;
 }
-// kind::f8f6f4, e4m3 operands, both K-major, float32 accumulator, M 128
-__host__ __device__ constexpr uint32_t a8_idesc(int N) { return (1u << 4) | (uint32_t)(N >> 3) << 17 | (128u >> 4) << 24; }
+// kind::f8f6f4, e4m3 operands, A K-major, B K-major or columns side by side, float32 accumulator, M 128
+__host__ __device__ constexpr uint32_t a8_idesc(int N, bool columns) {
+    return (1u << 4) | (columns ? 1u << 16 : 0u) | (uint32_t)(N >> 3) << 17 | (128u >> 4) << 24;
+}
 __device__ __forceinline__ void a8_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d),
                  "l"(a), "l"(b), "r"(idesc), "r"(acc)
@@ -124,6 +128,26 @@ __device__ __forceinline__ f2 add2(f2 x, f2 y) {
     f2 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
     return r;
+}
+
+// The nearest e4m3 of four floats as a word of codes; `rest`: what they leave, 16 times, in their place.
+__device__ __forceinline__ uint32_t a8_quad(f2 &x, f2 &y, bool rest) {
+    float x0, x1, y0, y1, f0, f1, g0, g1;
+    un2(x, x0, x1);
+    un2(y, y0, y1);
+    uint32_t w;
+    asm("{\n.reg .b16 a, b, c, d;\n.reg .b32 h;\n"
+        "cvt.rn.satfinite.e4m3x2.f32 a, %6, %5;\ncvt.rn.satfinite.e4m3x2.f32 b, %8, %7;\nmov.b32 %0, {a, b};\n"
+        "cvt.rn.f16x2.e4m3x2 h, a;\nmov.b32 {c, d}, h;\ncvt.f32.f16 %1, c;\ncvt.f32.f16 %2, d;\n"
+        "cvt.rn.f16x2.e4m3x2 h, b;\nmov.b32 {c, d}, h;\ncvt.f32.f16 %3, c;\ncvt.f32.f16 %4, d;\n}"
+        : "=r"(w), "=f"(f0), "=f"(f1), "=f"(g0), "=f"(g1)
+        : "f"(x0), "f"(x1), "f"(y0), "f"(y1));
+    if (rest) {
+        const f2 sixteen = mk2(16.f, 16.f), minus = mk2(-16.f, -16.f);
+        x = fma2(mk2(f0, f1), minus, mul2(x, sixteen));
+        y = fma2(mk2(g0, g1), minus, mul2(y, sixteen));
+    }
+    return w;
 }
 
 // Planes of QW queries from TMEM column `col` on, QT columns a plane: x = sum over planes of 16^-p plane p, in pairs
@@ -194,6 +218,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     int nr, base, c8;
     bool ok = true;
     if (a.seq_len) {
+        pdl_wait();   // everything that this call reads may come from the kernel before
         nr = a.n_rows[b];
         const int len = a.seq_len[b];
         const int64_t total = (int64_t)len + (a.advanced ? 0 : max(nr, 0));
@@ -357,7 +382,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
         }
         fence_async_smem();
     }
-    if (a.seq_len || warp >= W_MMA) pdl_wait();
+    if (warp >= W_MMA) pdl_wait();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -378,7 +403,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
         // warp in the loop, slots by division, a tile's two products took 1750 cycles to issue.
         if (tc_elect()) {
             const uint64_t dK = a8_desc(smem_u32(sk), 128, HD * 8), dQ = a8_desc(smem_u32(sqp), 128, HD * 8);
-            const uint64_t dV = a8_desc(smem_u32(sv), KB, 128), dP = a8_desc(smem_u32(spp), A8_PCH, 8 * A8_PCH);
+            const uint64_t dV = a8_desc(smem_u32(sv), KB, 128), dP = a8_desc(smem_u32(spp), 128, A8_PG);
             int ks = 0, kph = 0, vs = 0, vph = 0;   // slots and their phases
             auto scores = [&](int t) {   // of tile t: 128 keys x (planes x queries)
                 const int sb = NSB == 2 ? t & 1 : 0;
@@ -388,7 +413,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < HD / 32; ++k)
-                    a8_mma(tmem + sb * C::SC, dK + (ks * TB + k * 256) / 16, dQ + k * 16, a8_idesc(C::SC), k > 0);
+                    a8_mma(tmem + sb * C::SC, dK + (ks * TB + k * 256) / 16, dQ + k * 16, a8_idesc(C::SC, false), k > 0);
                 tc_commit(&sfull[sb]);
                 tc_commit(&kfree[ks]);
                 if (++ks == NS) ks = 0, kph ^= 1;
@@ -405,9 +430,9 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
                 if (n >= 4) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        a8_mma(tm_o, dV + (vs * TB + k * 2 * KB) / 16, dP + k * (2 * A8_PCH / 16), a8_idesc(C::OC), k > 0);
+                        a8_mma(tm_o, dV + (vs * TB + k * 2 * KB) / 16, dP + k * 32, a8_idesc(C::OC, true), k > 0);
                 } else
-                    for (int k = 0; k < n; ++k) a8_mma(tm_o, dV + (vs * TB + k * 2 * KB) / 16, dP + k * (2 * A8_PCH / 16), a8_idesc(C::OC), k > 0);
+                    for (int k = 0; k < n; ++k) a8_mma(tm_o, dV + (vs * TB + k * 2 * KB) / 16, dP + k * 32, a8_idesc(C::OC, true), k > 0);
                 tc_commit(&ofull);
                 tc_commit(&vfree[vs]);
                 if (++vs == NS) vs = 0, vph ^= 1;
@@ -497,7 +522,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
         }
         const uint32_t lanes = (uint32_t)(ww * 32) << 16;
         const int first_pos = base + (i0 >> lg);
-        const f2 down = mk2(1.f / A8_UP, 1.f / A8_UP), sixteen = mk2(16.f, 16.f), minus = mk2(-16.f, -16.f);
+        const f2 down = mk2(1.f / A8_UP, 1.f / A8_UP);
         for (int t = 0; t < nt; ++t) {
             const float ks = ksn, vs = vsn;
             scales(t + 1);
@@ -540,7 +565,8 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
             // the first tile sets the references too (the tail's may be far below)
             float top = e[0];
 #pragma unroll
-            for (int q = 1; q < QW; ++q) top = fmaxf(top, e[q]);
+            for (int q = 1; q + 1 < QW; q += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(e[q]), "f"(e[q + 1]));
+            top = fmaxf(top, e[QW - 1]);
             const bool over = a8_vote(bar, top > (t == 0 ? -INFINITY : A8_OVER));
             if (t > 0) {   // the output of the tile before: a thread is a dim
                 wait(&ofull, t - 1);
@@ -581,27 +607,24 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
                     }
                 named_sync(bar, 128);
             }
-            // weights, as planes
-            uint8_t *dst = spp + (wt >> 4) * A8_PCH + (wt & 15);
+            // weights, as planes: column n of key k at group n / 16, then k, then n % 16
+            uint8_t *dst = spp + wt * 16;
             const f2 rv2 = mk2(rvs, rvs), fv2 = mk2(fvs, fvs);
+            f2 x[QH];
 #pragma unroll
             for (int q = 0; q < QH; ++q) {
-                f2 x = mk2(a8_ex2(e[2 * q]), a8_ex2(e[2 * q + 1]));
-                l2[q] = fma2(x, rv2, l2[q]);
-                x = mul2(x, fv2);
+                x[q] = mk2(a8_ex2(e[2 * q]), a8_ex2(e[2 * q + 1]));
+                l2[q] = fma2(x[q], rv2, l2[q]);
+                x[q] = mul2(x[q], fv2);
+            }
 #pragma unroll
-                for (int p = 0; p < PP; ++p) {
-                    const int r = p * QT + q0 + 2 * q;
-                    float x0, x1;
-                    un2(x, x0, x1);
-                    const uint32_t c = e4m3x2(x0, x1);
-                    dst[(r >> 3) * (8 * A8_PCH) + (r & 7) * 16] = (uint8_t)c;
-                    dst[(r >> 3) * (8 * A8_PCH) + (r & 7) * 16 + 16] = (uint8_t)(c >> 8);
-                    if (p + 1 < PP) {
-                        const float2 f = e4m3x2_f(c);
-                        x = fma2(mk2(f.x, f.y), minus, mul2(x, sixteen));
-                    }
-                }
+            for (int p = 0; p < PP; ++p) {
+                uint32_t w[QH / 2];
+#pragma unroll
+                for (int q = 0; q < QH; q += 2) w[q / 2] = a8_quad(x[q], x[q + 1], p + 1 < PP);
+                const int n = p * QT + q0;
+                if constexpr (QW == 8) *(uint2 *)(dst + (n >> 4) * A8_PG + (n & 15)) = make_uint2(w[0], w[1]);
+                else *(uint32_t *)(dst + (n >> 4) * A8_PG + (n & 15)) = w[0];
             }
             // an odd number of pages: the reduction's last 16 keys are no one's, and 0 x anything has to be 0
             if ((n & 1) && tid < KB / 16) *(uint4 *)(sv + t % NS * TB + n * KB + tid * 16) = make_uint4(0, 0, 0, 0);
@@ -717,7 +740,7 @@ static cudaError_t launch_attn8_t(const Attn8Args &a, int sms, cudaStream_t s) {
     attr[0].val.clusterDim.x = cs;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = a.seq_len == nullptr;   // behind a draft call's own kernels
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     e = cudaLaunchKernelEx(&cfg, attn8_kernel<C>, a, tiles);
