@@ -179,13 +179,13 @@ int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv, int layer,
  *           smallest power of two, at least 2^-100, with max |x| <= 448 scale; NaN
  *           (and codes 0) for a block with a value that is not finite, so that
  *           every output that sees a key of the block is NaN.  Attention takes any
- *           positive scale.
+ *           positive scale, V's up to 2^40.
  *   k_tail, v_tail [n_layers][B][tail_pages][n_kv_heads][16][head_dim] bf16:
  *           position t of sequence b in ring page (t / 16) % tail_pages, slot t % 16
  *   page_table, seq_len, max_pages_per_seq, n_pages as osprey_kv
  *   tail_pages >= 1.  A caller may take back the last 16 * (tail_pages - 1)
- *           positions of a sequence by lowering seq_len: their page's rows are
- *           still in the tail. */
+ *           positions of a sequence by lowering seq_len (or by not advancing it):
+ *           the rows of the page that is unfinished then are still in the tail. */
 typedef struct osprey_kv8 {
     void *k8, *v8;
     float *k_scale, *v_scale;
@@ -214,8 +214,9 @@ int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, in
  *   out [B][max_rows][n_q_heads][head_dim] of q's type, 16-byte aligned; rows from
  *          n_rows[b] on are left as they were
  * Sums and softmax statistics are float32; q and the weights enter the tensor
- * cores as e4m3 planes that keep 8 (q) and 12 to 16 (weights) significant bits of
- * bf16 calls, 24 of float32 ones.  No workspace.
+ * cores as e4m3 planes: bf16 queries exactly (rotated ones to 12 significant bits or
+ * more) and their weights to 12 or more, float32 queries and weights to 24.  No
+ * workspace.
  * Device errors: INVALID_ARG (n_rows[b] outside 0 .. max_rows, or more than T),
  * CAPACITY (T past the page table, a page id out of range); such a sequence's
  * output rows are 0.

@@ -55,6 +55,7 @@ struct osprey_ctx {
     CUtensorMap tm_c, tm_lm, tm_qkv[OSPREY_MAX_LAYERS], tm_o[OSPREY_MAX_LAYERS], tm_gate[OSPREY_MAX_LAYERS],
         tm_up[OSPREY_MAX_LAYERS], tm_down[OSPREY_MAX_LAYERS];
     double inv_freq[64];
+    uint64_t turn_freq[64];   // inv_freq / 2 pi as a 64-bit fraction of a turn a position
     int n_probe;
     int probe_kind;   // OSPREY_PROBE_LM_HEAD or OSPREY_PROBE_ATTENTION
     cudaEvent_t *probe_begin, *probe_end;
@@ -129,6 +130,8 @@ extern "C" int osprey_create(const osprey_config *cfg, const osprey_weights *w, 
                     c.vocab, c.feat_dim, c.page_size, c.rms_eps};
     for (int i = 0; i < c.head_dim / 2; ++i)
         ctx->inv_freq[i] = std::pow((double)c.rope_theta, -2.0 * i / c.head_dim);
+    for (int i = 0; i < c.head_dim / 2; ++i)
+        ctx->turn_freq[i] = (uint64_t)std::ldexp(ctx->inv_freq[i] * 0.15915494309189535, 64);
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ctx->sms, cudaDevAttrMultiProcessorCount, dev);
@@ -371,12 +374,6 @@ extern "C" int osprey_kv_append(const osprey_ctx *ctx, const osprey_kv *kv, int 
 }
 
 // ------------------------------------------------------------------ appending with the rotation, the 8-bit cache
-// A rotary frequency as a 64-bit fraction of a turn for each position.
-static void rope_freqs(const osprey_ctx *ctx, uint64_t (&freq)[64]) {
-    for (int i = 0; i < ctx->dim.hd / 2; ++i)
-        freq[i] = (uint64_t)std::ldexp(ctx->inv_freq[i] * 0.15915494309189535, 64);
-}
-
 // What both appending calls check and pass on.
 static int kv_rope_args(const osprey_ctx *ctx, int layer, int B, const int32_t *n_rows, int64_t total_rows,
                         const void *k_rows, const void *v_rows, int rows_dtype, int64_t row_stride,
@@ -412,7 +409,7 @@ static int kv_rope_args(const osprey_ctx *ctx, int layer, int B, const int32_t *
     a.max_pages = max_pages;
     a.n_pages = n_pages;
     a.status = status;
-    rope_freqs(ctx, a.freq);
+    std::copy(ctx->turn_freq, ctx->turn_freq + 64, a.freq);
     return OSPREY_OK;
 }
 
@@ -519,7 +516,7 @@ extern "C" int osprey_kv8_attend(const osprey_ctx *ctx, const osprey_kv8 *kv, in
     a.q_f32 = dtype == OSPREY_F32;
     a.rotate = rotate != 0;
     a.q_stride = q_stride;
-    rope_freqs(ctx, a.freq);
+    std::copy(ctx->turn_freq, ctx->turn_freq + 64, a.freq);
     a.out = out;
     a.status = dev_status;
     const cudaError_t e = launch_attn8(a, ctx->sms, (cudaStream_t)stream);
@@ -556,6 +553,7 @@ static int draft_step_impl(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, i
         if (rc != OSPREY_OK) return rc;
         if (!draft_args_ok(ctx, B, K, max_new, kv8->max_pages_per_seq))
             return fail(OSPREY_ERR_INVALID_ARG, "K and max_new in 1..64, max_pages_per_seq >= 1 required");
+        if ((long long)B * kv8->tail_pages > INT32_MAX) return fail(OSPREY_ERR_INVALID_ARG, "B * tail_pages above 2^31 - 1");
         if (14 + max_new + K > 16LL * kv8->tail_pages)
             return fail(OSPREY_ERR_CAPACITY, "the tail's ring must hold an unfinished page and the call's rows: %d positions",
                         14 + max_new + K);

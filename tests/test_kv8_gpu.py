@@ -460,3 +460,133 @@ def test_decoding_with_the_cache(graph):
             # a key that rounds to the other bf16 or e4m3 neighbour, a query of 8 bits: percents of a weight
             assert np.abs(_dbl(out[b]) - want).max() <= 0.05 * np.abs(vs).max()
     assert int(st.item()) == 0 and kv.seq_len.tolist() == lens.tolist()
+
+
+def test_blocks_of_unlike_scales():
+    """A block of zeros and one of 2^-90 under most of the weight, and blocks of 2^30 beside them."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    for dtype in (BF, F32):
+        ctx = kc.make_ctx(4, 2, 128)
+        gen = torch.Generator(device="cuda").manual_seed(3)
+        kv, st = _cache(ctx, 1, 32, 5)
+        k, v = (kc.rows(gen, (1, 300, 2, 128), BF) for _ in range(2))
+        q = kc.rows(gen, (1, 1, 4, 128), dtype)
+        k[0, 32:64] = q[0, 0, ::2].to(BF)        # high scores
+        v[0, 32:48] = 0
+        v[0, 48:64] *= 2.0 ** -90
+        v[0, 100:200] *= 2.0 ** 30
+        ob.osprey_kv8_append(ctx, kv, _ints([300]), k, v, st, rotate=False)
+        out = torch.zeros_like(q)
+        ob.osprey_kv8_attend(ctx, kv, 0, _ints([1]), q, out, st)
+        torch.cuda.synchronize()
+        _check(q, out, [1], [300], _seen(k[0], [300]), _seen(v[0], [300]), dtype, 0.0)
+
+
+def test_values_next_to_a_page_that_is_no_ones():
+    """The slots behind an odd number of pages hold NaN codes of another sequence's page (0 x NaN must not appear)."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(4, 2, 128)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lens = [16 * 8 * 4, 16 * 5, 16, 16 * 9]
+    kv, st = _cache(ctx, 4, 64, 5)
+    k, v = _fill(ctx, kv, st, lens, gen)
+    q = kc.rows(gen, (4, 1, 4, 128), BF)
+    out = torch.zeros_like(q)
+    for _ in range(3):       # shared memory holds what the last call left
+        ob.osprey_kv8_attend(ctx, kv, 0, _ints([1] * 4), q, out, st)
+    torch.cuda.synchronize()
+    _check(q, out, [1] * 4, lens, _seen(k[0], lens), _seen(v[0], lens), BF, 0.0)
+
+
+def test_captured_behind_a_memset_and_beside_another_graph():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 4, 64)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lens = [77, 300]
+    kv, st = _cache(ctx, 2, 24, 5)
+    _fill(ctx, kv, st, lens, gen)
+    q = kc.rows(gen, (2, 2, 8, 64), BF)
+    want = torch.zeros_like(q)
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints([2, 2]), q, want, st)
+    n, outs, graphs = _ints([2, 2]), [torch.zeros_like(q) for _ in range(2)], []
+    torch.cuda.synchronize()
+    for o in outs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            o.zero_()
+            ob.osprey_kv8_attend(ctx, kv, 0, n, q, o, st)
+        graphs.append(g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        graphs[0].replay()
+        with torch.cuda.stream(side):
+            graphs[1].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], want) and int(st.item()) == 0
+
+
+def test_refusals():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 4, 64, 2)
+    kv, st = _cache(ctx, 2, 4, 5)
+    n = _ints([1, 1])
+    q = torch.zeros((2, 1, 8, 64), dtype=BF, device="cuda")
+    rows = torch.zeros((2, 2, 4, 64), dtype=BF, device="cuda")
+
+    def code(f, *a, **kw):
+        with pytest.raises(ob.OspreyError) as e:
+            f(*a, **kw)
+        return e.value.code
+
+    assert code(ob.osprey_kv8_attend, ctx, kv, 2, n, q, q.clone(), st) == -1
+    assert code(ob.osprey_kv8_attend, ctx, kv, -1, n, q, q.clone(), st) == -1
+    big = torch.zeros((2, 65, 8, 64), dtype=BF, device="cuda")
+    assert code(ob.osprey_kv8_attend, ctx, kv, 0, n, big, big.clone(), st) == -1
+    assert code(ob.osprey_kv8_append, ctx, kv, n, rows[0], rows[0], st, layer=5) == -1
+    # rows off 16 bytes, rows that overlap, another type, another shape
+    wide = torch.zeros((2, 2, 4 * 64 + 4), dtype=BF, device="cuda")[..., 4:].unflatten(-1, (4, 64))
+    assert code(ob.osprey_kv8_append, ctx, kv, n, wide, wide, st) == -1
+    for bad in (rows[:1, :1].expand(2, 2, 4, 64), rows.transpose(1, 2).contiguous().transpose(1, 2)):
+        with pytest.raises(ValueError):
+            ob.osprey_kv8_append(ctx, kv, n, bad, bad, st)
+    with pytest.raises(TypeError):
+        ob.osprey_kv8_append(ctx, kv, n, rows.half(), rows.half(), st)
+    with pytest.raises(ValueError):
+        ob.osprey_kv8_append(ctx, kv, n, rows, rows[:, :1], st)
+    with pytest.raises(ValueError):
+        ob.osprey_kv8_append(ctx, kv, n, rows[0], rows[0], st)          # one layer's rows for all layers
+    with pytest.raises(ValueError):
+        ob.osprey_kv8_attend(ctx, kv, 0, n, q.cpu(), q, st)
+    with pytest.raises(TypeError):
+        ob.osprey_kv8_attend(ctx, kv, 0, n, q, q.float(), st)
+    kv.k_scale = kv.k_scale[:, :-1].contiguous()
+    with pytest.raises(ValueError):
+        ob.osprey_kv8_attend(ctx, kv, 0, n, q, q.clone(), st)
+    # the C calls' own checks
+    import ctypes
+    kv2, _ = _cache(ctx, 2, 4, 5)
+    s = kv2.c_struct(ctx.shape)
+    call = lambda **kw: ob._c_kv8_attend(ctx.handle, ctypes.byref(s), *[  # noqa: E731
+        {**dict(layer=0, B=2, rows=1, n=n.data_ptr(), q=q.data_ptr(), dt=1, stride=0, rot=0, adv=1, out=q.data_ptr(),
+                st=st.data_ptr(), stream=None), **kw}[k]
+        for k in ("layer", "B", "rows", "n", "q", "dt", "stride", "rot", "adv", "out", "st", "stream")])
+    assert call(dt=7) == -3 and call(B=4097) == -1 and call(B=-1) == -1 and call(n=None) == -1 and call(out=None) == -1
+    assert call(stride=8) == -1 and call(stride=8 * 64 + 4) == -1 and call(q=q.data_ptr() + 2) == -1 and call(rows=0) == -1
+    assert call(B=0) == 0
+    for field in ("k8", "v_tail", "page_table", "seq_len"):
+        t = ob.osprey_kv8.from_buffer_copy(s)
+        setattr(t, field, None)
+        assert ob._c_kv8_attend(ctx.handle, ctypes.byref(t), 0, 2, 1, n.data_ptr(), q.data_ptr(), 1, 0, 0, 1, q.data_ptr(),
+                                st.data_ptr(), None) == -1
+    for field, v in (("tail_pages", 0), ("n_pages", 0), ("max_pages_per_seq", 1 << 26), ("k8", s.k8 + 8)):
+        t = ob.osprey_kv8.from_buffer_copy(s)
+        setattr(t, field, v)
+        assert ob._c_kv8_append(ctx.handle, ctypes.byref(t), 0, 2, n.data_ptr(), 2, rows.data_ptr(), rows.data_ptr(), 1, 0, 1,
+                                1, st.data_ptr(), None) == -1
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
