@@ -9,8 +9,9 @@
 
 namespace osp {
 
-constexpr int KR_THREADS = 256;
+constexpr int KR_THREADS = 128;
 constexpr int KR_WARPS = KR_THREADS / 32;
+constexpr int PK_THREADS = 256;   // of kv8_pack_kernel
 
 // Exclusive prefixes of two int64 a thread over the block, and their sums.
 __device__ __forceinline__ void kr_scan(int64_t &x, int64_t &y, int64_t (*sh)[2], int64_t &sum_x, int64_t &sum_y) {
@@ -159,10 +160,10 @@ __device__ __forceinline__ void kv8_rows_v(uint32_t (&x)[KvBlock<HD>::W], T *pag
 // once (fixed-point turns, then sincospif) and shared by its warps, which take K or V
 // of one layer and head at a time through registers: rows are read once, rotated, and
 // written in bf16 (to the page, or to the tail) or, where the page is finished,
-// as codes.  A warp's first rows are on their way while the angles are made.  Units
+// as codes; where units are few, several blocks (grid y) share one's layers and heads.  A warp's first rows are on their way while the angles are made.  Units
 // are found by a scan over the batch that each block keeps in registers.
 template <int HD, bool EIGHT, bool RF32>
-__global__ void __launch_bounds__(KR_THREADS, RF32 ? 2 : 3) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
+__global__ void __launch_bounds__(KR_THREADS, RF32 ? 4 : 5) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
     __shared__ int64_t sh[KR_WARPS][2];
     __shared__ __align__(16) float2 cs[16][HD / 2];   // pairs of dims e, e + 1 of chunk c at (e / 2) C + c: lanes side by side
     __shared__ int s_b, s_page, s_L0, s_n;
@@ -284,7 +285,8 @@ __global__ void __launch_bounds__(KR_THREADS, RF32 ? 2 : 3) kv_rope_kernel(const
                 }
             };
             if (pass == 1) __syncthreads();   // p0's older rows are read, and so are its angles
-            if (warp < items) fetch(warp);
+            const int it0 = warp + blockIdx.y * KR_WARPS;
+            if (it0 < items) fetch(it0);
             if (a.rotate && work)
                 for (int i = threadIdx.x; i < (t1 - t0) * (HD / 2); i += KR_THREADS) {
                     const int t = t0 + i / (HD / 2), d = i % (HD / 2);
@@ -292,12 +294,12 @@ __global__ void __launch_bounds__(KR_THREADS, RF32 ? 2 : 3) kv_rope_kernel(const
                     rope_cs_fix(a.freq[d], p * 16 + t, w.x, w.y);
                 }
             __syncthreads();
-            for (int it = warp; it < items; it += KR_WARPS) {
+            for (int it = it0; it < items; it += KR_WARPS * gridDim.y) {
                 const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv, layer = a.layer0 + l;
                 const size_t blk = ((size_t)layer * a.n_pages + page) * a.Hkv + h;
                 // this page's bf16 rows: the tail's, or the page's own
                 const size_t at = (EIGHT ? (((size_t)layer * a.B + b) * TP + p % TP) * a.Hkv + h : blk) * 16 * HD;
-                if (it != warp) fetch(it);
+                if (it != it0) fetch(it);
                 if ((it & 1) == 0) {
 #pragma unroll
                     for (int i = 0; i < Blk::NK; ++i) {
@@ -356,8 +358,10 @@ static cudaError_t launch_kv_rope_t(const KvRopeArgs &a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     // units: n rows touch at most n / 16 + 2 pages, and no more pages than rows
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.total_rows, a.total_rows / 16 + 2LL * a.B));
-    const int64_t cap = (RF32 ? 2LL : 3LL) * sms;   // as many as are resident
-    kv_rope_kernel<HD, EIGHT, RF32><<<(unsigned)std::min(most, cap), KR_THREADS, 0, s>>>(a);
+    const int64_t cap = (RF32 ? 4LL : 5LL) * sms;   // as many as are resident
+    // few units: up to four blocks share one's layers and heads
+    const int share = most * 4 <= cap && 2 * a.layers * a.Hkv > 2 * KR_WARPS ? 4 : most * 2 <= cap && 2 * a.layers * a.Hkv > KR_WARPS ? 2 : 1;
+    kv_rope_kernel<HD, EIGHT, RF32><<<dim3((unsigned)std::min(most, cap), share), KR_THREADS, 0, s>>>(a);
     count_launch();
     return cudaGetLastError();
 }
@@ -387,13 +391,13 @@ cudaError_t launch_kv_rope(const KvRopeArgs &a, bool eight, bool advance, cudaSt
 // Finished pages of a draft call's committed rows, from the tail: one warp K or V of a
 // layer and head, one block a page.
 template <int HD>
-__global__ void __launch_bounds__(KR_THREADS) kv8_pack_kernel(const Kv8PackArgs a) {
+__global__ void __launch_bounds__(PK_THREADS) kv8_pack_kernel(const Kv8PackArgs a) {
     const int b = blockIdx.y, warp = threadIdx.x >> 5;
     if (!a.valid[b]) return;
     const int p = a.pos0[b] / 16 + blockIdx.x;
     if ((p + 1) * 16 > a.pos0[b] + a.nnew[b]) return;
     const int page = a.page_table[(size_t)b * a.max_pages + p];   // in range: the call's first kernel has checked it
-    for (int it = warp; it < 2 * a.L * a.Hkv; it += KR_WARPS) {
+    for (int it = warp; it < 2 * a.L * a.Hkv; it += PK_THREADS / 32) {
         const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
         const size_t t = ((((size_t)l * a.B + b) * a.tail_pages + p % a.tail_pages) * a.Hkv + h) * 16 * HD;
         const size_t blk = ((size_t)l * a.n_pages + page) * a.Hkv + h;
@@ -410,8 +414,8 @@ __global__ void __launch_bounds__(KR_THREADS) kv8_pack_kernel(const Kv8PackArgs 
 
 cudaError_t launch_kv8_pack(const Kv8PackArgs &a, cudaStream_t s) {
     const dim3 grid((a.max_new + 14) / 16 + 1, a.B);   // pages that max_new rows finish, at most
-    if (a.hd == 128) kv8_pack_kernel<128><<<grid, KR_THREADS, 0, s>>>(a);
-    else kv8_pack_kernel<64><<<grid, KR_THREADS, 0, s>>>(a);
+    if (a.hd == 128) kv8_pack_kernel<128><<<grid, PK_THREADS, 0, s>>>(a);
+    else kv8_pack_kernel<64><<<grid, PK_THREADS, 0, s>>>(a);
     count_launch();
     return cudaGetLastError();
 }
