@@ -748,14 +748,23 @@ static cudaError_t launch_attn8_t(const Attn8Args &a, int sms, cudaStream_t s) {
     return e;
 }
 
+// A block takes as many queries as a call can have of one sequence and KV head (rows x
+// heads of a group), up to 8 with two blocks an SM.  More go 16 at a time, two blocks an
+// SM, up to 32 of them, else 32 at a time: a block of 32 has the SM to itself.  Numbers of
+// rows mostly differ from sequence to sequence, and blocks of 16 leave fewer warps idle
+// where they do.  us a call, 16 / 32 at a time: 1..8 rows of 96 sequences, groups of four
+// 160 / 183; 1..16 rows of 64, groups of two 77 / 91; 8 rows of each of 32 sequences,
+// groups of four 93 / 83, 4 rows 51 / 68, 16 rows 162 / 157; 50..64 rows of 8 205 / 187.
+// Float32 queries take twice the planes.
 template <int HD>
 static cudaError_t launch_attn8_h(const Attn8Args &a, int sms, cudaStream_t s) {
     const int nq = a.max_rows * (a.Hq / a.Hkv);
     if (a.q_f32) return nq <= 4 ? launch_attn8_t<A8<HD, 4, 4, 6, 6, 2, 3>>(a, sms, s) : launch_attn8_t<A8<HD, 8, 8, 6, 6, 2, 2>>(a, sms, s);
     if (nq <= 4) return launch_attn8_t<A8<HD, 4, 4, 4, 4, 2, 3>>(a, sms, s);
     if (nq <= 8) return launch_attn8_t<A8<HD, 8, 8, 4, 4, 2, 3>>(a, sms, s);
-    if (a.rotate) return launch_attn8_t<A8<HD, 32, 8, 3, 3, 1, 4>>(a, sms, s);
-    return launch_attn8_t<A8<HD, 32, 8, 2, 3, 1, 4>>(a, sms, s);
+    // a rotated bf16 query has more bits than its type: three planes keep 12
+    if (nq <= 32) return a.rotate ? launch_attn8_t<A8<HD, 16, 8, 3, 3, 2, 2>>(a, sms, s) : launch_attn8_t<A8<HD, 16, 8, 2, 3, 2, 3>>(a, sms, s);
+    return a.rotate ? launch_attn8_t<A8<HD, 32, 8, 3, 3, 1, 4>>(a, sms, s) : launch_attn8_t<A8<HD, 32, 8, 2, 3, 1, 4>>(a, sms, s);
 }
 
 cudaError_t launch_attn8(const Attn8Args &a, int sms, cudaStream_t s) {
