@@ -207,7 +207,8 @@ int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, in
  *          position T - n_rows[b] + j and sees the positions up to its own, T =
  *          seq_len[b] (advanced 1) or seq_len[b] + n_rows[b] (advanced 0: the
  *          rows are appended, the length is not).  Their K/V rows are in the cache.
- *   max_rows 1 .. 64
+ *   max_rows 1 .. 65536, B * max_rows * n_q_heads at most 2^28 (a decode step's row, what
+ *          a verification accepted, a prompt)
  *   q [B][max_rows] rows of [n_q_heads][head_dim], q_stride elements apart (0:
  *          dense), OSPREY_BF16 or OSPREY_F32; rotate 1: turned to their positions
  *          on the way.  Rows start on 16 bytes.

@@ -496,7 +496,8 @@ extern "C" int osprey_kv8_attend(const osprey_ctx *ctx, const osprey_kv8 *kv, in
     const Dims &D = ctx->dim;
     if (B < 0 || B > 4096) return fail(OSPREY_ERR_INVALID_ARG, "B must be in 0..4096");
     if (layer < 0 || layer >= D.L) return fail(OSPREY_ERR_INVALID_ARG, "layer must be in 0..%d", D.L - 1);
-    if (max_rows < 1 || max_rows > 64) return fail(OSPREY_ERR_INVALID_ARG, "max_rows must be in 1..64");
+    if (max_rows < 1 || max_rows > 65536 || (long long)B * max_rows * D.Hq > (1LL << 28))
+        return fail(OSPREY_ERR_INVALID_ARG, "max_rows must be in 1..65536, B * max_rows * n_q_heads at most 2^28");
     if (dtype != OSPREY_F32 && dtype != OSPREY_BF16) return fail(OSPREY_ERR_DTYPE, "unknown dtype %d", dtype);
     const int rc = kv8_check(kv);
     if (rc != OSPREY_OK) return rc;

@@ -271,6 +271,24 @@ def test_many_rows(Hq, Hkv, hd, dtype, rows):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+def test_prompts(dtype):
+    """Whole prompts, one of them behind a cached prefix: every row sees what is before it."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(4, 2, 64)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n, lens = [333, 200, 1, 0], [333, 500, 1, 90]
+    kv, st = _cache(ctx, 4, 40, 5)
+    k, v = _fill(ctx, kv, st, lens, gen)
+    q = kc.rows(gen, (4, 333, 4, 64), dtype)
+    out = torch.full_like(q, 9.0)
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints(n), q, out, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    _check(q, out, n, lens, _seen(k[0], lens), _seen(v[0], lens), dtype, 9.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_peaked_scores(dtype):
     """Scores of tens to hundreds: the maximum moves from key to key, and small weights vanish."""
     import kv8_cases as kc
@@ -545,8 +563,9 @@ def test_refusals():
 
     assert code(ob.osprey_kv8_attend, ctx, kv, 2, n, q, q.clone(), st) == -1
     assert code(ob.osprey_kv8_attend, ctx, kv, -1, n, q, q.clone(), st) == -1
-    big = torch.zeros((2, 65, 8, 64), dtype=BF, device="cuda")
+    big = torch.zeros((2, 65537, 8, 64), dtype=BF, device="cuda")
     assert code(ob.osprey_kv8_attend, ctx, kv, 0, n, big, big.clone(), st) == -1
+    del big
     assert code(ob.osprey_kv8_append, ctx, kv, n, rows[0], rows[0], st, layer=5) == -1
     # rows off 16 bytes, rows that overlap, another type, another shape
     wide = torch.zeros((2, 2, 4 * 64 + 4), dtype=BF, device="cuda")[..., 4:].unflatten(-1, (4, 64))
