@@ -218,9 +218,12 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     int nr, base, c8;
     bool ok = true;
     if (a.seq_len) {
-        pdl_wait();   // everything that this call reads may come from the kernel before
-        nr = a.n_rows[b];
-        const int len = a.seq_len[b];
+        // Everything that this call reads may come from the kernel before, which this one may
+        // have started beside: it is read through L2, and by the copies after a proxy fence.
+        pdl_wait();
+        asm volatile("fence.proxy.async.global;" ::: "memory");
+        nr = __ldcg(a.n_rows + b);
+        const int len = __ldcg(a.seq_len + b);
         const int64_t total = (int64_t)len + (a.advanced ? 0 : max(nr, 0));
         ok = nr >= 0 && nr <= a.max_rows && len >= 0 && total >= nr && total <= (int64_t)a.max_pages * 16;
         if (!ok && rank == 0 && tid == 0)
@@ -270,7 +273,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
         }
         __syncwarp();
     };
-    auto lane_id = [&](int t) { return lane < 8 && t * 8 + lane < np ? __ldg(tab + t * 8 + lane) : 0; };
+    auto lane_id = [&](int t) { return lane < 8 && t * 8 + lane < np ? __ldcg(tab + t * 8 + lane) : 0; };
     int ids = 0;   // of the next tile to ask for
     if (warp == W_MMA) {
         if (lane == 0) {
@@ -308,12 +311,12 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     // compute threads: the thread's key of tile t; its page's scales are loaded a tile ahead, the page's id two
     const int wt = tid & 127;
     float ksn = 0.f, vsn = 1.f;
-    auto key_id = [&](int t) { return t * 8 + (wt >> 4) < np ? __ldg(tab + t * 8 + (wt >> 4)) : 0; };
+    auto key_id = [&](int t) { return t * 8 + (wt >> 4) < np ? __ldcg(tab + t * 8 + (wt >> 4)) : 0; };
     auto scales = [&](int t) {
         if (t * 8 + (wt >> 4) < np) {
             const size_t blk = block_of(ids);
-            ksn = __ldg(a.k_scale + blk);
-            vsn = __ldg(a.v_scale + blk);
+            ksn = __ldcg(a.k_scale + blk);
+            vsn = __ldcg(a.v_scale + blk);
         }
     };
     const bool tail = ok && rank == cs - 1;

@@ -157,7 +157,7 @@ __device__ __forceinline__ void kv8_rows_v(uint32_t (&x)[KvBlock<HD>::W], T *pag
 
 // Bound by memory for prompts, by latency for a decode step.  A unit is one page of
 // one sequence, for all layers and heads: the angles of its new positions are made
-// once (fixed-point turns, then sincospif) and shared by its warps, which take K or V
+// once and shared by its warps, which take K or V
 // of one layer and head at a time through registers: rows are read once, rotated, and
 // written in bf16 (to the page, or to the tail) or, where the page is finished,
 // as codes; where units are few, several blocks (grid y) share one's layers and heads.  A warp's first rows are on their way while the angles are made.  Units
