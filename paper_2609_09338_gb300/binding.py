@@ -265,8 +265,9 @@ class Kv8Cache:
     page_table: torch.Tensor   # [B, max_pages] int32
     seq_len: torch.Tensor      # [B] int32
 
-    def __post_init__(self):
-        self._key = self._struct = None
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_checked", None)
 
     @property
     def max_pages(self) -> int:
@@ -281,30 +282,27 @@ class Kv8Cache:
         return self.k_tail.shape[1] // max(1, self.page_table.shape[0])
 
     def c_struct(self, shape: DrafterShape) -> osprey_kv8:
-        """The C struct, after the checks of the tensors against the drafter's shape (made again when a tensor's
-        memory or size is not what it was at the last call)."""
+        """The C struct.  The tensors are checked against the drafter's shape when one of them, or its size, is
+        another than at the check before."""
         k8, v8, ks, vs, kt, vt = self.k8, self.v8, self.k_scale, self.v_scale, self.k_tail, self.v_tail
         tab, n = self.page_table, self.seq_len
-        key = (shape, k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), kt.data_ptr(), vt.data_ptr(),
-               tab.data_ptr(), n.data_ptr(), k8.numel(), v8.numel(), ks.numel(), vs.numel(), kt.numel(), vt.numel(),
-               tab.shape, n.numel())
-        if key == self._key:
-            return self._struct
-        L, H, hd = shape.n_layers, shape.n_kv_heads, shape.head_dim
-        _need(tab, torch.int32, None, "page_table")
-        if tab.dim() != 2 or k8.dim() != 4:
-            raise ValueError("page_table is [B, max_pages], k8 [L, n_pages, Hkv, 16 * hd]")
-        B, pages, t = tab.shape[0], self.n_pages, self.tail_pages
-        _need(k8, torch.uint8, (L, pages, H, 16 * hd), "k8")
-        _need(v8, torch.uint8, (L, pages, H, 16 * hd), "v8")
-        _need(ks, torch.float32, (L, pages, H), "k_scale")
-        _need(vs, torch.float32, (L, pages, H), "v_scale")
-        _need(kt, torch.bfloat16, (L, B * t, H, 16, hd), "k_tail")
-        _need(vt, torch.bfloat16, (L, B * t, H, 16, hd), "v_tail")
-        _need(n, torch.int32, (B,), "seq_len")
-        self._struct = osprey_kv8(*key[1:9], self.max_pages, pages, t)
-        self._key = key
-        return self._struct
+        sizes = (shape, k8.numel(), v8.numel(), ks.numel(), vs.numel(), kt.numel(), vt.numel(), tab.shape, n.numel())
+        if self._checked is None or self._checked[0] != sizes:
+            L, H, hd = shape.n_layers, shape.n_kv_heads, shape.head_dim
+            _need(tab, torch.int32, None, "page_table")
+            if tab.dim() != 2 or k8.dim() != 4:
+                raise ValueError("page_table is [B, max_pages], k8 [L, n_pages, Hkv, 16 * hd]")
+            B, pages, t = tab.shape[0], self.n_pages, self.tail_pages
+            _need(k8, torch.uint8, (L, pages, H, 16 * hd), "k8")
+            _need(v8, torch.uint8, (L, pages, H, 16 * hd), "v8")
+            _need(ks, torch.float32, (L, pages, H), "k_scale")
+            _need(vs, torch.float32, (L, pages, H), "v_scale")
+            _need(kt, torch.bfloat16, (L, B * t, H, 16, hd), "k_tail")
+            _need(vt, torch.bfloat16, (L, B * t, H, 16, hd), "v_tail")
+            _need(n, torch.int32, (B,), "seq_len")
+            object.__setattr__(self, "_checked", (sizes, (tab.shape[1], pages, t)))
+        return osprey_kv8(k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), kt.data_ptr(), vt.data_ptr(),
+                          tab.data_ptr(), n.data_ptr(), *self._checked[1])
 
 
 def alloc_kv8(shape: DrafterShape, page_table: np.ndarray, n_pages: int, tail_pages: int = 2, device="cuda") -> Kv8Cache:

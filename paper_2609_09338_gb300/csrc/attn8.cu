@@ -106,30 +106,6 @@ __device__ __forceinline__ void a8_ld(uint32_t addr, float *v) {
     for (int j = 0; j < N; ++j) v[j] = __uint_as_float(r[j]);
 }
 
-// Two floats an instruction.
-typedef unsigned long long f2;
-__device__ __forceinline__ f2 mk2(float x, float y) {
-    f2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void un2(f2 v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ f2 fma2(f2 x, f2 y, f2 z) {
-    f2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
-    return r;
-}
-__device__ __forceinline__ f2 mul2(f2 x, f2 y) {
-    f2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-__device__ __forceinline__ f2 add2(f2 x, f2 y) {
-    f2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
-}
-
 // The nearest e4m3 of four floats as a word of codes; `rest`: what they leave, 16 times, in their place.
 __device__ __forceinline__ uint32_t a8_quad(f2 &x, f2 &y, bool rest) {
     float x0, x1, y0, y1, f0, f1, g0, g1;

@@ -38,6 +38,10 @@ __device__ __forceinline__ void kr_scan(int64_t &x, int64_t &y, int64_t (*sh)[2]
 // Pages that n rows after L0 touch.
 __device__ __forceinline__ int kr_pages(int L0, int n) { return n > 0 ? (L0 + n - 1) / 16 - L0 / 16 + 1 : 0; }
 
+__device__ __forceinline__ void cp16(void *dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+
 // One warp's block of one page and head (K or V) in registers, 16 rows x HD as bf16 pairs.
 // K: the lane's items are (row, 8 dims, the 8 dims hd / 2 further), the halves that the
 // rotation mixes.  V: the lane holds HD / 32 dims of all 16 rows, so that it can write
@@ -51,12 +55,26 @@ struct KvBlock {
     static constexpr int W = 16 * NV;       // words of a lane's share, of K too (8 an iteration: low, then high half)
 };
 
+// max(m, |x|) of a pair of bf16; a NaN stays (its bits are above infinity's)
+__device__ __forceinline__ uint32_t bf2_max_abs(uint32_t m, uint32_t x) {
+    uint32_t r;
+    asm("{\n.reg .b32 t;\nabs.bf16x2 t, %2;\nmax.NaN.bf16x2 %0, %1, t;\n}" : "=r"(r) : "r"(m), "r"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf2_mul(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// 2^-e twice in bf16: a block's values times it are exact, or under the least code's half
+__device__ __forceinline__ uint32_t kv8_inv2(int e) { return (uint32_t)(127 - e) << 7 | (uint32_t)(127 - e) << 23; }
+
 // The block's scale: its exponent (0 for a block with an infinity or a NaN, *bad)
 template <int W>
 __device__ __forceinline__ int kv8_scale(const uint32_t (&x)[W], float *scale, bool &bad) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < W; ++i) m = __vmaxu2(m, x[i] & 0x7fff7fffu);
+    for (int i = 0; i < W; ++i) m = bf2_max_abs(m, x[i]);
     m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
     bad = m >= 0x7f80u;
     const int e = bad ? 0 : kv8_exp(m);
@@ -70,7 +88,7 @@ __device__ __forceinline__ void kv8_quantise_k(const uint32_t (&x)[KvBlock<HD>::
     using B = KvBlock<HD>;
     const int lane = threadIdx.x & 31, c = lane % B::C;
     bool bad;
-    const float inv = kv8_pow2(-kv8_scale(x, scale, bad));
+    const uint32_t inv = kv8_inv2(kv8_scale(x, scale, bad));
 #pragma unroll
     for (int i = 0; i < B::NK; ++i) {
         const int r = lane / B::C + i * B::RPI;
@@ -79,8 +97,8 @@ __device__ __forceinline__ void kv8_quantise_k(const uint32_t (&x)[KvBlock<HD>::
             uint32_t w[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const uint32_t u = x[8 * i + 4 * half + 2 * j], v = x[8 * i + 4 * half + 2 * j + 1];
-                w[j] = e4m3x2(bf_lo(u) * inv, bf_hi(u) * inv) | e4m3x2(bf_lo(v) * inv, bf_hi(v) * inv) << 16;
+                const uint32_t u = bf2_mul(x[8 * i + 4 * half + 2 * j], inv), v = bf2_mul(x[8 * i + 4 * half + 2 * j + 1], inv);
+                w[j] = e4m3x4(bf_lo(u), bf_hi(u), bf_lo(v), bf_hi(v));
             }
             const int d = half * (HD / 2) + c * 8;
             *(uint2 *)(dst + ((r >> 3) * (HD / 16) + (d >> 4)) * 128 + (r & 7) * 16 + (d & 15)) =
@@ -95,7 +113,10 @@ __device__ __forceinline__ void kv8_quantise_v(const uint32_t (&x)[KvBlock<HD>::
     using B = KvBlock<HD>;
     const int lane = threadIdx.x & 31;
     bool bad;
-    const float inv = kv8_pow2(-kv8_scale(x, scale, bad));
+    const uint32_t inv = kv8_inv2(kv8_scale(x, scale, bad));
+    uint32_t y[B::W];
+#pragma unroll
+    for (int i = 0; i < B::W; ++i) y[i] = bf2_mul(x[i], inv);
 #pragma unroll
     for (int j = 0; j < B::NV; ++j)
 #pragma unroll
@@ -103,8 +124,8 @@ __device__ __forceinline__ void kv8_quantise_v(const uint32_t (&x)[KvBlock<HD>::
             uint32_t w[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                auto val = [&](int t) { return (h ? bf_hi(x[t * B::NV + j]) : bf_lo(x[t * B::NV + j])) * inv; };
-                w[g] = e4m3x2(val(4 * g), val(4 * g + 1)) | e4m3x2(val(4 * g + 2), val(4 * g + 3)) << 16;
+                auto val = [&](int t) { return h ? bf_hi(y[t * B::NV + j]) : bf_lo(y[t * B::NV + j]); };
+                w[g] = e4m3x4(val(4 * g), val(4 * g + 1), val(4 * g + 2), val(4 * g + 3));
             }
             *(uint4 *)(dst + (lane * (HD / 32) + 2 * j + h) * 16) =
                 bad ? make_uint4(0, 0, 0, 0) : make_uint4(w[0], w[1], w[2], w[3]);
@@ -155,17 +176,30 @@ __device__ __forceinline__ void kv8_rows_v(uint32_t (&x)[KvBlock<HD>::W], T *pag
     }
 }
 
-// Bound by memory for prompts, by latency for a decode step.  A unit is one page of
-// one sequence, for all layers and heads: the angles of its new positions are made
-// once and shared by its warps, which take K or V
-// of one layer and head at a time through registers: rows are read once, rotated, and
-// written in bf16 (to the page, or to the tail) or, where the page is finished,
-// as codes; where units are few, several blocks (grid y) share one's layers and heads.  A warp's first rows are on their way while the angles are made.  Units
-// are found by a scan over the batch that each block keeps in registers.
+// Blocks an SM.  float32 rows come through registers, twice as many as bf16 ones: with
+// three blocks (160 registers) nothing is spilled; four took 9.3 us instead of 7.5 for 1..8
+// rows of 96 sequences in 8 bits, 47 instead of 43 for 17 k rows of two layers.
+template <int HD, bool RF32>
+constexpr int kr_blocks = RF32 ? (HD == 128 ? 3 : 4) : 5;
+
+// A unit is one page of one sequence, for all layers and heads: the angles of its new
+// positions are made once and shared by its warps, which take K or V of one layer and head
+// at a time through registers: rows are read once, rotated, and written in bf16 (to the
+// page, or to the tail) or, where the page is finished, as codes.  bf16 rows come by way of
+// shared memory, a warp's next ones while it works on these.  Where units are few, several
+// blocks (grid y) share one's layers and heads.  Units are found by a scan over the batch
+// that each block keeps in registers.
+//
+// 33 k rows of 16 sequences, two layers of 4 heads of 128, with the lengths' update: to the
+// bf16 cache 50 us, 5.5 TB/s, bound by memory (0.81 of a plain copy's rate); to the 8-bit
+// one 46 us, 4.4 TB/s, bound by issue slots (some 900 instructions a 4 KB block: unpack,
+// turn, round, maximum, scale, round).  A decode step (one row of 64 sequences) takes 4.2
+// and 5.4 us: the chain of lengths, page, rows and angles.
 template <int HD, bool EIGHT, bool RF32>
-__global__ void __launch_bounds__(KR_THREADS, RF32 ? 4 : 5) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
+__global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
     __shared__ int64_t sh[KR_WARPS][2];
-    __shared__ __align__(16) float2 cs[16][HD / 2];   // pairs of dims e, e + 1 of chunk c at (e / 2) C + c: lanes side by side
+    __shared__ float4 cs[16][HD / 4];   // cos, cos, sin, sin of dims e, e + 1 of chunk c at (e / 2) C + c: lanes side by side
+    __shared__ __align__(16) uint16_t stage[RF32 ? 1 : KR_WARPS][2][RF32 ? 8 : 16 * HD];   // a warp's rows, and its next ones
     __shared__ int s_b, s_page, s_L0, s_n;
     __shared__ int64_t s_row;
     using Blk = KvBlock<HD>;
@@ -257,15 +291,6 @@ __global__ void __launch_bounds__(KR_THREADS, RF32 ? 4 : 5) kv_rope_kernel(const
 #pragma unroll
                             for (int j = 0; j < 4; ++j) *(uint4 *)(f + 16 * i + 4 * j) = __ldg(src + (j >> 1) * (HD / 8) + (j & 1));
                         }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < Blk::NK; ++i) {
-                            const int r = lane / Blk::C + i * Blk::RPI;
-                            if (r < t0 || r >= t1) continue;
-                            const uint16_t *src = (const uint16_t *)a.k_rows + at0 + r * a.row_stride + lane % Blk::C * 8;
-                            *(uint4 *)(x + 8 * i) = ld_stream(src);
-                            *(uint4 *)(x + 8 * i + 4) = ld_stream(src + HD / 2);
-                        }
                     }
                 } else {
 #pragma unroll
@@ -276,30 +301,56 @@ __global__ void __launch_bounds__(KR_THREADS, RF32 ? 4 : 5) kv_rope_kernel(const
                             const float *src = (const float *)a.v_rows + at;
                             if constexpr (HD == 128) *(uint4 *)(f + 4 * t) = __ldg((const uint4 *)src);
                             else *(uint2 *)(f + 2 * t) = __ldg((const uint2 *)src);
-                        } else {
-                            const uint16_t *src = (const uint16_t *)a.v_rows + at;
-                            if constexpr (HD == 128) *(uint2 *)(x + 2 * t) = __ldg((const uint2 *)src);
-                            else x[t] = __ldg((const uint32_t *)src);
                         }
                     }
                 }
             };
+            // bf16 rows come by way of shared memory, the next item's while this one's are worked on
+            auto ask = [&](int it, int slot) {
+                const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
+                const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;
+                const uint16_t *src = (const uint16_t *)(it & 1 ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
+                uint16_t *dst = &stage[warp][slot][0];
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i) {
+                    const int j = lane + 32 * i, r = j / (HD / 8), d = j % (HD / 8) * 8;
+                    if (r >= t0 && r < t1) cp16(dst + r * HD + d, src + r * a.row_stride + d);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
             if (pass == 1) __syncthreads();   // p0's older rows are read, and so are its angles
             const int it0 = warp + blockIdx.y * KR_WARPS;
-            if (it0 < items) fetch(it0);
+            const int step = KR_WARPS * gridDim.y;
+            if (it0 < items) {
+                if constexpr (RF32) fetch(it0);
+                else ask(it0, 0);
+            }
             if (a.rotate && work)
                 for (int i = threadIdx.x; i < (t1 - t0) * (HD / 2); i += KR_THREADS) {
                     const int t = t0 + i / (HD / 2), d = i % (HD / 2);
-                    float2 &w = cs[t][((d >> 1 & 3) * Blk::C + (d >> 3)) * 2 + (d & 1)];
-                    rope_cs_fix(a.freq[d], p * 16 + t, w.x, w.y);
+                    float *w = (float *)&cs[t][(d >> 1 & 3) * Blk::C + (d >> 3)] + (d & 1);
+                    rope_cs_fix(a.freq[d], p * 16 + t, w[0], w[2]);
                 }
             __syncthreads();
-            for (int it = it0; it < items; it += KR_WARPS * gridDim.y) {
+            int slot = 0;
+            for (int it = it0; it < items; it += step, slot ^= 1) {
                 const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv, layer = a.layer0 + l;
                 const size_t blk = ((size_t)layer * a.n_pages + page) * a.Hkv + h;
                 // this page's bf16 rows: the tail's, or the page's own
                 const size_t at = (EIGHT ? (((size_t)layer * a.B + b) * TP + p % TP) * a.Hkv + h : blk) * 16 * HD;
-                if (it != it0) fetch(it);
+                if constexpr (RF32) {
+                    if (it != it0) fetch(it);
+                } else {
+                    __syncwarp();   // the slot has been read
+                    if (it + step < items) {
+                        ask(it + step, slot ^ 1);
+                        asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    } else
+                        asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    __syncwarp();
+                    if ((it & 1) == 0) kv8_rows_k<HD, false>(x, &stage[warp][slot][0], 0, 16);
+                    else kv8_rows_v<HD, false>(x, &stage[warp][slot][0], 0, 16);
+                }
                 if ((it & 1) == 0) {
 #pragma unroll
                     for (int i = 0; i < Blk::NK; ++i) {
@@ -315,13 +366,10 @@ __global__ void __launch_bounds__(KR_THREADS, RF32 ? 4 : 5) kv_rope_kernel(const
                                 v[k] = RF32 ? __uint_as_float(f[(RF32 ? 16 * i + 8 + e + k : 0)]) : k ? bf_hi(hi) : bf_lo(hi);
                             }
                             if (a.rotate) {
-                                const float4 w = *(const float4 *)&cs[r][(e / 2 * Blk::C + lane % Blk::C) * 2];
-#pragma unroll
-                                for (int k = 0; k < 2; ++k) {
-                                    const float c = k ? w.z : w.x, s = k ? w.w : w.y, y = u[k] * c - v[k] * s;
-                                    v[k] = v[k] * c + u[k] * s;
-                                    u[k] = y;
-                                }
+                                const float4 w = cs[r][e / 2 * Blk::C + lane % Blk::C];
+                                const f2 c = mk2(w.x, w.y), u2 = mk2(u[0], u[1]), v2 = mk2(v[0], v[1]);
+                                un2(fma2(v2, mk2(-w.z, -w.w), mul2(u2, c)), u[0], u[1]);
+                                un2(fma2(u2, mk2(w.z, w.w), mul2(v2, c)), v[0], v[1]);
                             }
                             lo = kv8_bf2(u[0], u[1]);
                             hi = kv8_bf2(v[0], v[1]);
@@ -330,7 +378,7 @@ __global__ void __launch_bounds__(KR_THREADS, RF32 ? 4 : 5) kv_rope_kernel(const
                     uint16_t *bf = (EIGHT ? a.k_tail : a.k_pages) + at;
                     if (!EIGHT || tail) kv8_rows_k<HD, true>(x, bf, t0, t1);
                     if (full) {
-                        kv8_rows_k<HD, false>(x, bf, 0, t0);   // older rows (t0 > 0: p is p0, its own ring page)
+                        if (t0 > 0) kv8_rows_k<HD, false>(x, bf, 0, t0);   // older rows (t0 > 0: p is p0, its own ring page)
                         kv8_quantise_k<HD>(x, a.k8 + blk * 16 * HD, a.k_scale + blk);
                     }
                 } else {
@@ -340,7 +388,7 @@ __global__ void __launch_bounds__(KR_THREADS, RF32 ? 4 : 5) kv_rope_kernel(const
                     uint16_t *bf = (EIGHT ? a.v_tail : a.v_pages) + at;
                     if (!EIGHT || tail) kv8_rows_v<HD, true>(x, bf, t0, t1);
                     if (full) {
-                        kv8_rows_v<HD, false>(x, bf, 0, t0);
+                        if (t0 > 0) kv8_rows_v<HD, false>(x, bf, 0, t0);
                         kv8_quantise_v<HD>(x, a.v8 + blk * 16 * HD, a.v_scale + blk);
                     }
                 }
@@ -358,10 +406,15 @@ static cudaError_t launch_kv_rope_t(const KvRopeArgs &a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     // units: n rows touch at most n / 16 + 2 pages, and no more pages than rows
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.total_rows, a.total_rows / 16 + 2LL * a.B));
-    const int64_t cap = (RF32 ? 4LL : 5LL) * sms;   // as many as are resident
+    const int64_t cap = kr_blocks<HD, RF32> * (int64_t)sms;   // as many as are resident
     // few units: up to four blocks share one's layers and heads
     const int share = most * 4 <= cap && 2 * a.layers * a.Hkv > 2 * KR_WARPS ? 4 : most * 2 <= cap && 2 * a.layers * a.Hkv > KR_WARPS ? 2 : 1;
-    kv_rope_kernel<HD, EIGHT, RF32><<<dim3((unsigned)std::min(most, cap), share), KR_THREADS, 0, s>>>(a);
+    // More units than that: a block takes several in a row; but one where a unit is little more
+    // than its copy (bf16) and finding it is cheap (up to four sequences a thread).  us, one a
+    // block / several: bf16, 16 sequences 50.0 / 53.7, 100 43.3 / 45.3, 512 50.2 / 53.1, 2048
+    // 74 / 47; 8 bits, 16 sequences 47.3 / 46.4, 2048 91 / 65.
+    const int64_t most_blocks = (!EIGHT && a.B <= 4 * KR_THREADS ? 16 : 1) * cap;
+    kv_rope_kernel<HD, EIGHT, RF32><<<dim3((unsigned)std::min(most, most_blocks), share), KR_THREADS, 0, s>>>(a);
     count_launch();
     return cudaGetLastError();
 }

@@ -51,6 +51,30 @@ __device__ __forceinline__ void rope_cs_fix(uint64_t freq, int pos, float &c, fl
     if (q & 2) s = -s;
 }
 
+// Two floats an instruction.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 mk2(float x, float y) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void un2(f2 v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ f2 fma2(f2 x, f2 y, f2 z) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 x, f2 y) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 x, f2 y) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+
 // bf16(x1) : bf16(x0), rounded to nearest even; NaN stays NaN
 __device__ __forceinline__ uint32_t kv8_bf2(float x0, float x1) {
     uint32_t r;
@@ -61,6 +85,13 @@ __device__ __forceinline__ uint32_t kv8_bf2(float x0, float x1) {
 __device__ __forceinline__ uint32_t e4m3x2(float x0, float x1) {
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(x1), "f"(x0));
+    return r;
+}
+// four of them, the first in the low byte
+__device__ __forceinline__ uint32_t e4m3x4(float x0, float x1, float x2, float x3) {
+    uint32_t r;
+    asm("{\n.reg .b16 a, b;\ncvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\ncvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\nmov.b32 %0, {a, b};\n}"
+        : "=r"(r) : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
     return r;
 }
 // the two values of a pair of codes

@@ -609,3 +609,26 @@ def test_refusals():
                                 1, st.data_ptr(), None) == -1
     torch.cuda.synchronize()
     assert int(st.item()) == 0
+
+
+def test_a_tensor_put_into_the_cache_later_is_checked_and_used():
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(8, 4, 64, 2)
+    kv, st = _cache(ctx, 2, 4, 5)
+    n = _ints([1, 1])
+    rows = torch.ones((2, 2, 4, 64), dtype=BF, device="cuda")
+    ob.osprey_kv8_append(ctx, kv, n, rows, rows, st)
+    kept = kv.k_tail
+    kv.k_tail = torch.zeros_like(kept, dtype=torch.int16)
+    with pytest.raises(TypeError):
+        ob.osprey_kv8_append(ctx, kv, n, rows, rows, st)
+    kv.k_tail = kept
+    kept = kv.seq_len
+    kv.seq_len = _ints([1, 1, 1])
+    with pytest.raises(ValueError):
+        ob.osprey_kv8_append(ctx, kv, n, rows, rows, st)
+    kv.seq_len = _ints([3, 5])
+    ob.osprey_kv8_append(ctx, kv, n, rows, rows, st)
+    torch.cuda.synchronize()
+    assert kv.seq_len.tolist() == [4, 6] and kept.tolist() == [1, 1] and int(st.item()) == 0
