@@ -192,8 +192,8 @@ constexpr int kr_blocks = RF32 ? (HD == 128 ? 3 : 4) : 5;
 //
 // 33 k rows of 16 sequences, two layers of 4 heads of 128, with the lengths' update: to the
 // bf16 cache 50 us, 5.5 TB/s, bound by memory (0.81 of a plain copy's rate); to the 8-bit
-// one 46 us, 4.4 TB/s, bound by issue slots (some 900 instructions a 4 KB block: unpack,
-// turn, round, maximum, scale, round).  A decode step (one row of 64 sequences) takes 4.2
+// one 46 us, 4.4 TB/s, bound by its instructions (some 950 a 4 KB block: unpack, turn,
+// round, maximum, scale, round) and the barriers between pages.  A decode step (one row of 64 sequences) takes 4.2
 // and 5.4 us: the chain of lengths, page, rows and angles.
 template <int HD, bool EIGHT, bool RF32>
 __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
@@ -275,32 +275,30 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
             const bool full = EIGHT && pass == 0 && t1 == 16, work = !EIGHT || full || tail;
             const int page = tab[p], items = work ? 2 * a.layers * a.Hkv : 0;
             __align__(16) uint32_t x[Blk::W], f[RF32 ? 2 * Blk::W : 1];   // the lane's share of the block; float32 rows as they come
+            // float32 rows, to registers
             auto fetch = [&](int it) {
-                const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
-                const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;   // row of slot 0
-                const int64_t at0 = first * a.row_stride + h * HD;
+                if constexpr (RF32) {
+                    const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
+                    const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;   // row of slot 0
+                    const float *src = (const float *)(it & 1 ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
 #pragma unroll
-                for (int i = 0; i < Blk::W; ++i) x[i] = 0;
-                if ((it & 1) == 0) {
-                    if constexpr (RF32) {
+                    for (int i = 0; i < 2 * Blk::W; ++i) f[i] = 0;
+                    if ((it & 1) == 0) {
 #pragma unroll
                         for (int i = 0; i < Blk::NK; ++i) {
                             const int r = lane / Blk::C + i * Blk::RPI;
                             if (r < t0 || r >= t1) continue;
-                            const uint4 *src = (const uint4 *)((const float *)a.k_rows + at0 + r * a.row_stride + lane % Blk::C * 8);
+                            const uint4 *at = (const uint4 *)(src + r * a.row_stride + lane % Blk::C * 8);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) *(uint4 *)(f + 16 * i + 4 * j) = __ldg(src + (j >> 1) * (HD / 8) + (j & 1));
+                            for (int j = 0; j < 4; ++j) *(uint4 *)(f + 16 * i + 4 * j) = __ldg(at + (j >> 1) * (HD / 8) + (j & 1));
                         }
-                    }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int t = 0; t < 16; ++t) {
-                        if (t < t0 || t >= t1) continue;
-                        const int64_t at = at0 + t * a.row_stride + lane * (HD / 32);
-                        if constexpr (RF32) {
-                            const float *src = (const float *)a.v_rows + at;
-                            if constexpr (HD == 128) *(uint4 *)(f + 4 * t) = __ldg((const uint4 *)src);
-                            else *(uint2 *)(f + 2 * t) = __ldg((const uint2 *)src);
+                        for (int t = 0; t < 16; ++t) {
+                            if (t < t0 || t >= t1) continue;
+                            const float *at = src + t * a.row_stride + lane * (HD / 32);
+                            if constexpr (HD == 128) *(uint4 *)(f + 4 * t) = __ldg((const uint4 *)at);
+                            else *(uint2 *)(f + 2 * t) = __ldg((const uint2 *)at);
                         }
                     }
                 }

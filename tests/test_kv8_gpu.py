@@ -632,3 +632,39 @@ def test_a_tensor_put_into_the_cache_later_is_checked_and_used():
     ob.osprey_kv8_append(ctx, kv, n, rows, rows, st)
     torch.cuda.synchronize()
     assert kv.seq_len.tolist() == [4, 6] and kept.tolist() == [1, 1] and int(st.item()) == 0
+
+
+@pytest.mark.parametrize("B", [2, 128, 130])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_more_blocks_than_the_device_takes_at_once(B, dtype):
+    """Equal lengths, sequences without rows and bad lengths among them."""
+    import kv8_cases as kc
+    from paper_2609_09338_gb300 import binding as ob
+    ctx = kc.make_ctx(16, 8, 64)
+    gen = torch.Generator(device="cuda").manual_seed(B)
+    rng = np.random.default_rng(B)
+    rows = 4 if B > 2 else 400
+    lens = [int(x) for x in rng.integers(rows, 450, B)]
+    n = [int(x) for x in rng.integers(0, rows + 1, B)]
+    lens[B // 2] = lens[0]
+    if B > 2:
+        lens[5:9] = [rows] * 4
+    kv, st = _cache(ctx, B, 32, 5)
+    k, v = _fill(ctx, kv, st, lens, gen)
+    q = kc.rows(gen, (B, rows, 16, 64), dtype)
+    out = torch.full_like(q, 9.0)
+    ob.osprey_kv8_attend(ctx, kv, 0, _ints(n), q, out, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    ks, vs = _seen(k[0], lens), _seen(v[0], lens)
+    _check(q, out, n, lens, ks, vs, dtype, 9.0)
+    if B > 2:   # a length that is none, and one past the page table
+        kv.seq_len[3] = -7
+        kv.seq_len[20] = 1 << 30
+        n[3] = n[20] = 2
+        again = torch.full_like(q, 9.0)
+        ob.osprey_kv8_attend(ctx, kv, 0, _ints(n), q, again, st)
+        torch.cuda.synchronize()
+        assert int(st.item()) in (-1, -4)
+        for b in range(B):
+            assert not again[b, :2].any() if b in (3, 20) else torch.equal(again[b], out[b]), b
