@@ -282,12 +282,12 @@ class Kv8Cache:
         return self.k_tail.shape[1] // max(1, self.page_table.shape[0])
 
     def c_struct(self, shape: DrafterShape) -> osprey_kv8:
-        """The C struct.  The tensors are checked against the drafter's shape when one of them, or its size, is
+        """The C struct.  The tensors are checked against the drafter's shape when one of them, or the batch, is
         another than at the check before."""
         k8, v8, ks, vs, kt, vt = self.k8, self.v8, self.k_scale, self.v_scale, self.k_tail, self.v_tail
         tab, n = self.page_table, self.seq_len
-        sizes = (shape, k8.numel(), v8.numel(), ks.numel(), vs.numel(), kt.numel(), vt.numel(), tab.shape, n.numel())
-        if self._checked is None or self._checked[0] != sizes:
+        checked = self._checked
+        if checked is None or checked[0] is not shape or checked[1] != tab.shape:
             L, H, hd = shape.n_layers, shape.n_kv_heads, shape.head_dim
             _need(tab, torch.int32, None, "page_table")
             if tab.dim() != 2 or k8.dim() != 4:
@@ -300,9 +300,10 @@ class Kv8Cache:
             _need(kt, torch.bfloat16, (L, B * t, H, 16, hd), "k_tail")
             _need(vt, torch.bfloat16, (L, B * t, H, 16, hd), "v_tail")
             _need(n, torch.int32, (B,), "seq_len")
-            object.__setattr__(self, "_checked", (sizes, (tab.shape[1], pages, t)))
+            checked = (shape, tab.shape, tab.shape[1], pages, t)
+            object.__setattr__(self, "_checked", checked)
         return osprey_kv8(k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), kt.data_ptr(), vt.data_ptr(),
-                          tab.data_ptr(), n.data_ptr(), *self._checked[1])
+                          tab.data_ptr(), n.data_ptr(), *checked[2:])
 
 
 def alloc_kv8(shape: DrafterShape, page_table: np.ndarray, n_pages: int, tail_pages: int = 2, device="cuda") -> Kv8Cache:
@@ -358,10 +359,10 @@ def _strided_rows(t, lead, inner, name):
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name} must be on the current device")
-    if tuple(t.shape) != (*lead, *inner):
+    if t.shape != (*lead, *inner):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(*lead, *inner)}")
     dense = inner[0] * inner[1]
-    if t.numel() == 0:
+    if t.is_contiguous():
         return dense
     st = t.stride()
     if (inner[1] > 1 and st[-1] != 1) or (inner[0] > 1 and st[-2] != inner[1]):

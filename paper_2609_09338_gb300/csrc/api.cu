@@ -427,7 +427,7 @@ extern "C" int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv,
         return fail(OSPREY_ERR_INVALID_ARG, "K/V pages must be given and 16-byte aligned");
     a.k_pages = (uint16_t *)kv->k_pages;
     a.v_pages = (uint16_t *)kv->v_pages;
-    const cudaError_t e = launch_kv_rope(a, false, advance != 0, (cudaStream_t)stream);
+    const cudaError_t e = launch_kv_rope(a, false, advance != 0, ctx->sms, (cudaStream_t)stream);
     return e == cudaSuccess ? OSPREY_OK : cuda_fail(e, "kv_append_rope launch");
 }
 
@@ -462,7 +462,7 @@ extern "C" int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, in
     a.k_tail = (uint16_t *)kv->k_tail;
     a.v_tail = (uint16_t *)kv->v_tail;
     a.tail_pages = kv->tail_pages;
-    const cudaError_t e = launch_kv_rope(a, true, advance != 0, (cudaStream_t)stream);
+    const cudaError_t e = launch_kv_rope(a, true, advance != 0, ctx->sms, (cudaStream_t)stream);
     return e == cudaSuccess ? OSPREY_OK : cuda_fail(e, "kv8_append launch");
 }
 

@@ -397,11 +397,7 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
 }
 
 template <int HD, bool EIGHT, bool RF32>
-static cudaError_t launch_kv_rope_t(const KvRopeArgs &a, cudaStream_t s) {
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
+static cudaError_t launch_kv_rope_t(const KvRopeArgs &a, int sms, cudaStream_t s) {
     // units: n rows touch at most n / 16 + 2 pages, and no more pages than rows
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(a.total_rows, a.total_rows / 16 + 2LL * a.B));
     const int64_t cap = kr_blocks<HD, RF32> * (int64_t)sms;   // as many as are resident
@@ -417,14 +413,14 @@ static cudaError_t launch_kv_rope_t(const KvRopeArgs &a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_kv_rope(const KvRopeArgs &a, bool eight, bool advance, cudaStream_t s) {
+cudaError_t launch_kv_rope(const KvRopeArgs &a, bool eight, bool advance, int sms, cudaStream_t s) {
     cudaError_t e;
     if (a.hd == 128)
-        e = eight ? (a.rows_f32 ? launch_kv_rope_t<128, true, true>(a, s) : launch_kv_rope_t<128, true, false>(a, s))
-                  : (a.rows_f32 ? launch_kv_rope_t<128, false, true>(a, s) : launch_kv_rope_t<128, false, false>(a, s));
+        e = eight ? (a.rows_f32 ? launch_kv_rope_t<128, true, true>(a, sms, s) : launch_kv_rope_t<128, true, false>(a, sms, s))
+                  : (a.rows_f32 ? launch_kv_rope_t<128, false, true>(a, sms, s) : launch_kv_rope_t<128, false, false>(a, sms, s));
     else
-        e = eight ? (a.rows_f32 ? launch_kv_rope_t<64, true, true>(a, s) : launch_kv_rope_t<64, true, false>(a, s))
-                  : (a.rows_f32 ? launch_kv_rope_t<64, false, true>(a, s) : launch_kv_rope_t<64, false, false>(a, s));
+        e = eight ? (a.rows_f32 ? launch_kv_rope_t<64, true, true>(a, sms, s) : launch_kv_rope_t<64, true, false>(a, sms, s))
+                  : (a.rows_f32 ? launch_kv_rope_t<64, false, true>(a, sms, s) : launch_kv_rope_t<64, false, false>(a, sms, s));
     if (e != cudaSuccess || !advance) return e;
     KvAppendArgs v{};
     v.page_table = a.page_table;

@@ -129,7 +129,7 @@ struct KvRopeArgs {
     uint16_t *k_tail, *v_tail;
     int tail_pages;
 };
-cudaError_t launch_kv_rope(const KvRopeArgs &a, bool eight, bool advance, cudaStream_t s);
+cudaError_t launch_kv_rope(const KvRopeArgs &a, bool eight, bool advance, int sms, cudaStream_t s);
 
 // Quantises the pages that positions pos0[b] .. pos0[b] + nnew[b] - 1 of valid
 // sequences finish, from the tail (every layer).
