@@ -82,6 +82,11 @@ __device__ __forceinline__ int kv8_scale(const uint32_t (&x)[W], float *scale, b
     return e;
 }
 
+template <int HD>
+__device__ __forceinline__ void kv8_zero(uint8_t *dst) {
+    for (int i = threadIdx.x & 31; i < HD; i += 32) *(uint4 *)(dst + i * 16) = make_uint4(0, 0, 0, 0);
+}
+
 // codes of a K block and its scale, from bf16 values
 template <int HD>
 __device__ __forceinline__ void kv8_quantise_k(const uint32_t (&x)[KvBlock<HD>::W], uint8_t *dst, float *scale) {
@@ -89,6 +94,7 @@ __device__ __forceinline__ void kv8_quantise_k(const uint32_t (&x)[KvBlock<HD>::
     const int lane = threadIdx.x & 31, c = lane % B::C;
     bool bad;
     const uint32_t inv = kv8_inv2(kv8_scale(x, scale, bad));
+    if (bad) return kv8_zero<HD>(dst);
 #pragma unroll
     for (int i = 0; i < B::NK; ++i) {
         const int r = lane / B::C + i * B::RPI;
@@ -102,7 +108,7 @@ __device__ __forceinline__ void kv8_quantise_k(const uint32_t (&x)[KvBlock<HD>::
             }
             const int d = half * (HD / 2) + c * 8;
             *(uint2 *)(dst + ((r >> 3) * (HD / 16) + (d >> 4)) * 128 + (r & 7) * 16 + (d & 15)) =
-                bad ? make_uint2(0, 0) : make_uint2(w[0], w[1]);
+                make_uint2(w[0], w[1]);
         }
     }
 }
@@ -114,6 +120,7 @@ __device__ __forceinline__ void kv8_quantise_v(const uint32_t (&x)[KvBlock<HD>::
     const int lane = threadIdx.x & 31;
     bool bad;
     const uint32_t inv = kv8_inv2(kv8_scale(x, scale, bad));
+    if (bad) return kv8_zero<HD>(dst);
     uint32_t y[B::W];
 #pragma unroll
     for (int i = 0; i < B::W; ++i) y[i] = bf2_mul(x[i], inv);
@@ -127,8 +134,7 @@ __device__ __forceinline__ void kv8_quantise_v(const uint32_t (&x)[KvBlock<HD>::
                 auto val = [&](int t) { return h ? bf_hi(y[t * B::NV + j]) : bf_lo(y[t * B::NV + j]); };
                 w[g] = e4m3x4(val(4 * g), val(4 * g + 1), val(4 * g + 2), val(4 * g + 3));
             }
-            *(uint4 *)(dst + (lane * (HD / 32) + 2 * j + h) * 16) =
-                bad ? make_uint4(0, 0, 0, 0) : make_uint4(w[0], w[1], w[2], w[3]);
+            *(uint4 *)(dst + (lane * (HD / 32) + 2 * j + h) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
         }
 }
 
@@ -223,6 +229,10 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
         return;
     }
     pdl_trigger();
+    // An item is K or V of a layer and head.  A warp takes K and V in turn (K, with its
+    // rotation, is twice V's work): of the items 2 i and 2 i + 1 the first is K in even rounds.
+    const int step = KR_WARPS * gridDim.y, step_log = __ffs(step) - 1;
+    auto is_v = [&](int it) { return (it + (it >> step_log)) & 1; };
     int last_b = -1;
     bool last_ok = false;
     // a contiguous range of the units: a sequence's pages are checked once a block
@@ -280,10 +290,10 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
                 if constexpr (RF32) {
                     const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
                     const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;   // row of slot 0
-                    const float *src = (const float *)(it & 1 ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
+                    const float *src = (const float *)(is_v(it) ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
 #pragma unroll
                     for (int i = 0; i < 2 * Blk::W; ++i) f[i] = 0;
-                    if ((it & 1) == 0) {
+                    if (!is_v(it)) {
 #pragma unroll
                         for (int i = 0; i < Blk::NK; ++i) {
                             const int r = lane / Blk::C + i * Blk::RPI;
@@ -307,7 +317,7 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
             auto ask = [&](int it, int slot) {
                 const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
                 const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;
-                const uint16_t *src = (const uint16_t *)(it & 1 ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
+                const uint16_t *src = (const uint16_t *)(is_v(it) ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
                 uint16_t *dst = &stage[warp][slot][0];
 #pragma unroll
                 for (int i = 0; i < HD / 16; ++i) {
@@ -318,7 +328,6 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
             };
             if (pass == 1) __syncthreads();   // p0's older rows are read, and so are its angles
             const int it0 = warp + blockIdx.y * KR_WARPS;
-            const int step = KR_WARPS * gridDim.y;
             if (it0 < items) {
                 if constexpr (RF32) fetch(it0);
                 else ask(it0, 0);
@@ -346,10 +355,10 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
                     } else
                         asm volatile("cp.async.wait_group 0;" ::: "memory");
                     __syncwarp();
-                    if ((it & 1) == 0) kv8_rows_k<HD, false>(x, &stage[warp][slot][0], 0, 16);
+                    if (!is_v(it)) kv8_rows_k<HD, false>(x, &stage[warp][slot][0], 0, 16);
                     else kv8_rows_v<HD, false>(x, &stage[warp][slot][0], 0, 16);
                 }
-                if ((it & 1) == 0) {
+                if (!is_v(it)) {
 #pragma unroll
                     for (int i = 0; i < Blk::NK; ++i) {
                         const int r = lane / Blk::C + i * Blk::RPI;
@@ -449,7 +458,7 @@ __global__ void __launch_bounds__(PK_THREADS) kv8_pack_kernel(const Kv8PackArgs 
         const size_t t = ((((size_t)l * a.B + b) * a.tail_pages + p % a.tail_pages) * a.Hkv + h) * 16 * HD;
         const size_t blk = ((size_t)l * a.n_pages + page) * a.Hkv + h;
         __align__(16) uint32_t x[KvBlock<HD>::W];
-        if ((it & 1) == 0) {
+        if ((it + it / (PK_THREADS / 32)) % 2 == 0) {   // K and V in turn, as above
             kv8_rows_k<HD, false>(x, a.k_tail + t, 0, 16);
             kv8_quantise_k<HD>(x, a.k8 + blk * 16 * HD, a.k_scale + blk);
         } else {
