@@ -197,9 +197,9 @@ constexpr int kr_blocks = RF32 ? (HD == 128 ? 3 : 4) : 5;
 // that each block keeps in registers.
 //
 // 33 k rows of 16 sequences, two layers of 4 heads of 128, with the lengths' update: to the
-// bf16 cache 50 us, 5.5 TB/s, bound by memory (0.81 of a plain copy's rate); to the 8-bit
-// one 46 us, 4.4 TB/s, bound by its instructions (some 950 a 4 KB block: unpack, turn,
-// round, maximum, scale, round) and the barriers between pages.  A decode step (one row of 64 sequences) takes 4.2
+// bf16 cache 50 us, 5.5 TB/s, bound by memory (0.82 of a plain copy's rate); to the 8-bit
+// one 42 us, 4.9 TB/s (0.72), bound by its instructions (some 900 a 4 KB block: unpack,
+// turn, round, maximum, scale, round) and the barriers between pages.  A decode step (one row of 64 sequences) takes 4.2
 // and 5.4 us: the chain of lengths, page, rows and angles.
 template <int HD, bool EIGHT, bool RF32>
 __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
@@ -286,9 +286,8 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
             const int page = tab[p], items = work ? 2 * a.layers * a.Hkv : 0;
             __align__(16) uint32_t x[Blk::W], f[RF32 ? 2 * Blk::W : 1];   // the lane's share of the block; float32 rows as they come
             // float32 rows, to registers
-            auto fetch = [&](int it) {
+            auto fetch = [&](int it, int l, int h) {
                 if constexpr (RF32) {
-                    const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
                     const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;   // row of slot 0
                     const float *src = (const float *)(is_v(it) ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
 #pragma unroll
@@ -314,8 +313,7 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
                 }
             };
             // bf16 rows come by way of shared memory, the next item's while this one's are worked on
-            auto ask = [&](int it, int slot) {
-                const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv;
+            auto ask = [&](int it, int l, int h, int slot) {
                 const int64_t first = (int64_t)l * a.total_rows + row + (int64_t)p * 16 - L0;
                 const uint16_t *src = (const uint16_t *)(is_v(it) ? a.v_rows : a.k_rows) + first * a.row_stride + h * HD;
                 uint16_t *dst = &stage[warp][slot][0];
@@ -328,9 +326,10 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
             };
             if (pass == 1) __syncthreads();   // p0's older rows are read, and so are its angles
             const int it0 = warp + blockIdx.y * KR_WARPS;
+            int l = (it0 >> 1) / a.Hkv, h = (it0 >> 1) - l * a.Hkv;   // the item's layer and head
             if (it0 < items) {
-                if constexpr (RF32) fetch(it0);
-                else ask(it0, 0);
+                if constexpr (RF32) fetch(it0, l, h);
+                else ask(it0, l, h, 0);
             }
             if (a.rotate && work)
                 for (int i = threadIdx.x; i < (t1 - t0) * (HD / 2); i += KR_THREADS) {
@@ -341,16 +340,18 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
             __syncthreads();
             int slot = 0;
             for (int it = it0; it < items; it += step, slot ^= 1) {
-                const int lh = it >> 1, l = lh / a.Hkv, h = lh - l * a.Hkv, layer = a.layer0 + l;
+                const int layer = a.layer0 + l;
+                int next_l = l, next_h = h + (step >> 1);
+                while (next_h >= a.Hkv) next_h -= a.Hkv, ++next_l;
                 const size_t blk = ((size_t)layer * a.n_pages + page) * a.Hkv + h;
                 // this page's bf16 rows: the tail's, or the page's own
                 const size_t at = (EIGHT ? (((size_t)layer * a.B + b) * TP + p % TP) * a.Hkv + h : blk) * 16 * HD;
                 if constexpr (RF32) {
-                    if (it != it0) fetch(it);
+                    if (it != it0) fetch(it, l, h);
                 } else {
                     __syncwarp();   // the slot has been read
                     if (it + step < items) {
-                        ask(it + step, slot ^ 1);
+                        ask(it + step, next_l, next_h, slot ^ 1);
                         asm volatile("cp.async.wait_group 1;" ::: "memory");
                     } else
                         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -399,6 +400,8 @@ __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_ker
                         kv8_quantise_v<HD>(x, a.v8 + blk * 16 * HD, a.v_scale + blk);
                     }
                 }
+                l = next_l;
+                h = next_h;
             }
         }
         __syncthreads();   // cs and s_b are read
@@ -413,10 +416,11 @@ static cudaError_t launch_kv_rope_t(const KvRopeArgs &a, int sms, cudaStream_t s
     // few units: up to four blocks share one's layers and heads
     const int share = most * 4 <= cap && 2 * a.layers * a.Hkv > 2 * KR_WARPS ? 4 : most * 2 <= cap && 2 * a.layers * a.Hkv > KR_WARPS ? 2 : 1;
     // More units than that: a block takes several in a row; but one where a unit is little more
-    // than its copy (bf16) and finding it is cheap (up to four sequences a thread).  us, one a
-    // block / several: bf16, 16 sequences 50.0 / 53.7, 100 43.3 / 45.3, 512 50.2 / 53.1, 2048
-    // 74 / 47; 8 bits, 16 sequences 47.3 / 46.4, 2048 91 / 65.
-    const int64_t most_blocks = (!EIGHT && a.B <= 4 * KR_THREADS ? 16 : 1) * cap;
+    // than its copy (bf16) or made of small items (head_dim 64), and finding it is cheap (up to
+    // four sequences a thread).  us, one a block / several: bf16, 16 sequences 50.0 / 53.7, 100
+    // 43.3 / 45.3, 512 50.2 / 53.1, 2048 74 / 47; 8 bits, 16 sequences 44.0 / 42.2, of head_dim
+    // 64 54.6 / 60.1, 2048 91 / 65.
+    const int64_t most_blocks = ((!EIGHT || HD == 64) && a.B <= 4 * KR_THREADS ? 16 : 1) * cap;
     kv_rope_kernel<HD, EIGHT, RF32><<<dim3((unsigned)std::min(most, most_blocks), share), KR_THREADS, 0, s>>>(a);
     count_launch();
     return cudaGetLastError();
