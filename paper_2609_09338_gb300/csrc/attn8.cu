@@ -37,6 +37,7 @@
 #include <algorithm>
 
 #include "attn8.cuh"
+#include "attn8_forms.h"
 #include "internal.h"
 #include "tcgen05.cuh"
 #include "tma.cuh"
@@ -45,32 +46,9 @@ namespace osp {
 
 namespace cg = cooperative_groups;
 
-constexpr int A8_CH = 32;            // tail keys of a step
-constexpr int A8_PG = 2048;          // bytes of 16 weight columns of a tile
 constexpr float A8_LO = -40.f;       // smallest log2 of a V scale that moves the reference
 constexpr float A8_OVER = 4.f;       // a weight is at most 2^A8_OVER, times A8_UP an e4m3 number
 constexpr float A8_UP = 16.f;
-
-// QT queries a block, QW of them a warpgroup's (4 warps); QP and PP planes of a query and
-// of a weight; BPS blocks an SM, of NS slots of K and V each.
-template <int HD_, int QT_, int QW_, int QP_, int PP_, int BPS_, int NS_>
-struct A8 {
-    static constexpr int HD = HD_, QT = QT_, QW = QW_, QP = QP_, PP = PP_, BPS = BPS_, NS = NS_ * 128 / HD;
-    static constexpr int NWG = QT / QW, CT = NWG * 128;   // warpgroups that compute, their threads
-    static constexpr int THREADS = CT + 96;               // and three warps: products, K copies, V copies
-    static constexpr int KB = 16 * HD, TB = 8 * KB;       // bytes of a page, of a tile's slot
-    static constexpr int SC = (QP * QT + 15) / 16 * 16, OC = (PP * QT + 15) / 16 * 16;   // TMEM columns of scores, output
-    static constexpr int TM = 512 / BPS;                  // columns a block may take
-    static constexpr int NSB = 2 * SC + OC <= TM ? 2 : 1;
-    static constexpr int USED = NSB * SC + OC;
-    static constexpr int COLS = USED <= 32 ? 32 : USED <= 64 ? 64 : USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
-    static constexpr int QB = SC * HD;                    // bytes of q's planes
-    static constexpr int PW = A8_PG * (OC / 16);          // bytes of the weights' planes
-    static constexpr int PB = PW > QT * HD * 4 ? PW : QT * HD * 4;   // their place, q's for the tail
-    static constexpr int SMEM = 2 * NS * TB + QB + PB + QT * A8_CH * 4;
-    static_assert((QW == 4 || QW == 8) && COLS <= TM && QB + PB >= KB && QT % QW == 0, "operands");
-    static_assert(QT * HD * 4 <= NS * TB, "the merge's outputs take the K slots");
-};
 
 // Shared-memory matrix descriptor of an operand without swizzle.  K-major: core matrices
 // of 8 rows x 16 bytes, lbo bytes apart along the reduction, sbo along the rows.  The
@@ -748,12 +726,12 @@ static cudaError_t launch_attn8_t(const Attn8Args &a, int sms, cudaStream_t s) {
 template <int HD>
 static cudaError_t launch_attn8_h(const Attn8Args &a, int sms, cudaStream_t s) {
     const int nq = a.max_rows * (a.Hq / a.Hkv);
-    if (a.q_f32) return nq <= 4 ? launch_attn8_t<A8<HD, 4, 4, 6, 6, 2, 3>>(a, sms, s) : launch_attn8_t<A8<HD, 8, 8, 6, 6, 2, 2>>(a, sms, s);
-    if (nq <= 4) return launch_attn8_t<A8<HD, 4, 4, 4, 4, 2, 3>>(a, sms, s);
-    if (nq <= 8) return launch_attn8_t<A8<HD, 8, 8, 4, 4, 2, 3>>(a, sms, s);
+    if (a.q_f32) return nq <= 4 ? launch_attn8_t<A8_4F<HD>>(a, sms, s) : launch_attn8_t<A8_8F<HD>>(a, sms, s);
+    if (nq <= 4) return launch_attn8_t<A8_4<HD>>(a, sms, s);
+    if (nq <= 8) return launch_attn8_t<A8_8<HD>>(a, sms, s);
     // a rotated bf16 query has more bits than its type: three planes keep 12
-    if (nq <= 32) return a.rotate ? launch_attn8_t<A8<HD, 16, 8, 3, 3, 2, 2>>(a, sms, s) : launch_attn8_t<A8<HD, 16, 8, 2, 3, 2, 3>>(a, sms, s);
-    return a.rotate ? launch_attn8_t<A8<HD, 32, 8, 3, 3, 1, 4>>(a, sms, s) : launch_attn8_t<A8<HD, 32, 8, 2, 3, 1, 4>>(a, sms, s);
+    if (nq <= 32) return a.rotate ? launch_attn8_t<A8_16R<HD>>(a, sms, s) : launch_attn8_t<A8_16<HD>>(a, sms, s);
+    return a.rotate ? launch_attn8_t<A8_32R<HD>>(a, sms, s) : launch_attn8_t<A8_32<HD>>(a, sms, s);
 }
 
 cudaError_t launch_attn8(const Attn8Args &a, int sms, cudaStream_t s) {
