@@ -216,8 +216,11 @@ int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, in
  *          n_rows[b] on are left as they were
  * Sums and softmax statistics are float32; q and the weights enter the tensor
  * cores as e4m3 planes: bf16 queries exactly (rotated ones to 12 significant bits or
- * more) and their weights to 12 or more, float32 queries and weights to 24.  No
- * workspace.
+ * more), float32 queries to 24.  A weight is off by at most 2^-16 of itself (float32
+ * queries: 2^-24) or, if that is more, 2^-25 (2^-33) of the largest one that its row has
+ * in the 17 x 128 keys up to its own (each weight times its block's v_scale), which counts
+ * as 2^-40 of the row's largest at least: the weights behind a key that takes nearly all
+ * of a row's keep their bits, whatever their share.  No workspace.
  * Device errors: INVALID_ARG (n_rows[b] outside 0 .. max_rows, or more than T),
  * CAPACITY (T past the page table, a page id out of range); such a sequence's
  * output rows are 0.

@@ -20,16 +20,26 @@
 // weights' planes; then it is a dim, and adds the output of the tile before from TMEM to
 // registers in float32.  Weights are 2^(s - m) with a reference m that stays while no
 // score exceeds it by more than A8_OVER: then a tile needs one vote, and no maxima.
+// The planes have a last step of their own, 2^-25 of the reference for four, 2^-33 for
+// six, so the reference has to come down too: behind a key that takes nearly all of the
+// weight the others' are 2^-20 of it and less, and their sum may be the whole output (16 k
+// keys behind one of 0.99 and value 0: an output off by 1.5e-1 of itself with three planes
+// and no such step, 9e-3 with four).  In the third tile, every A8_RENEW from there, and in
+// the one behind a tile that raised it, the reference becomes the tile's maximum, however
+// low, down to 2^-A8_DROP of the largest: float32 holds sums that much larger than the
+// reference.  References are whole but the tail's, so sums are scaled by powers of two.
+// (One thread a query finds the new references, all read what it left: with each thread
+// finding all of them, which takes its registers, the many-row calls below took 187 and 229 us.)
 // The V block's scale goes into the weight, w' = 2^(s + log2(vs) - m); the sum adds
 // w' / vs.
 //
 // Measured (GB300, keys of 8 KV heads of 128).  One row of 64 sequences of 1024..16384
 // keys: 174 us, 6.55 TB/s, bound by memory (0.97 of a plain copy's rate).  Groups of four,
-// 1..8 rows of 96 sequences of 1024..4096 keys: 161 us; 50..64 rows of 8 sequences of
-// 2000..8192 keys: 187 us; these are bound by the arithmetic between the two products, 335
-// instructions a warp and tile (the tensor pipe is 14 % busy), and by a tile's chain.
+// 1..8 rows of 96 sequences of 1024..4096 keys: 173 us; 50..64 rows of 8 sequences of
+// 2000..8192 keys: 206 us (160 and 190 with three planes of the weights, 12 bits instead of
+// 16); these are bound by the arithmetic between the two products and by a tile's chain.
 // float32 queries, groups of four, 16 sequences of 2048..8192 keys of 4 heads: 26 us.  A
-// call of one sequence takes 6.7 us.  Taking sequences longest first (a ranking in each
+// call of one sequence takes 6.5 us.  Taking sequences longest first (a ranking in each
 // block) made the first 183 us, the second 163, and the third, which is 187 to 207 with
 // the sequences' order, 189: sequences are taken as they come.
 #include <cooperative_groups.h>
@@ -48,6 +58,8 @@ namespace cg = cooperative_groups;
 
 constexpr float A8_LO = -40.f;       // smallest log2 of a V scale that moves the reference
 constexpr float A8_OVER = 4.f;       // a weight is at most 2^A8_OVER, times A8_UP an e4m3 number
+constexpr float A8_DROP = 40.f;      // a reference is at least 2^-A8_DROP of the largest one so far
+constexpr int A8_RENEW = 16;         // tiles a reference stays at most
 constexpr float A8_UP = 16.f;
 
 // Shared-memory matrix descriptor of an operand without swizzle.  K-major: core matrices
@@ -171,8 +183,8 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     float *sp = (float *)(spp + C::PB);             // [QT][A8_CH] the tail's weights
     float *so = (float *)sk;                        // [QT][HD] at the end
     __shared__ __align__(8) uint64_t kfull[NS], vfull[NS], kfree[NS], vfree[NS], sfull[2], sread[1], pready, ofull;
-    __shared__ __align__(16) float s_red[C::NWG][4][QW], s_mul[QT], s_nref[QT], s_m[QT];
-    __shared__ float s_l[QT], s_corr[QT], s_lw[4][QT];
+    __shared__ __align__(16) float s_red[C::NWG][4][QW], s_mul[QT], s_nref[QT], s_m[QT], s_best[QT], s_corr[QT], s_by[QT];
+    __shared__ float s_l[QT], s_lw[4][QT];
     __shared__ int s_pos[QT], s_bad, s_abort;
     __shared__ uint32_t s_tmem;
     cg::cluster_group cluster = cg::this_cluster();
@@ -342,7 +354,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
             if (lane == 0) {
                 s_mul[q] = fin ? unit * kv8_pow2(-e) : __uint_as_float(0x7fffffffu);
                 s_pos[q] = base + j;
-                s_m[q] = -INFINITY;
+                s_m[q] = s_best[q] = -INFINITY;
                 s_nref[q] = 0.f;
                 s_l[q] = 0.f;
             }
@@ -458,7 +470,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
                     if (lane == 0) {
                         s_corr[q] = corr;
                         s_l[q] = s_l[q] * corr + ls;
-                        s_m[q] = mn;
+                        s_m[q] = s_best[q] = mn;
                         s_nref[q] = -ref;
                     }
                 }
@@ -490,6 +502,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
         const uint32_t lanes = (uint32_t)(ww * 32) << 16;
         const int first_pos = base + (i0 >> lg);
         const f2 down = mk2(1.f / A8_UP, 1.f / A8_UP);
+        bool raised = false;   // the tile before exceeded its references
         for (int t = 0; t < nt; ++t) {
             const float ks = ksn, vs = vsn;
             scales(t + 1);
@@ -529,12 +542,12 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
                 for (int q = 0; q < QW; ++q)
                     if (!in || key > s_pos[q0 + q]) e[q] = -INFINITY;
             }
-            // the first tile sets the references too (the tail's may be far below)
             float top = e[0];
 #pragma unroll
             for (int q = 1; q + 1 < QW; q += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(e[q]), "f"(e[q + 1]));
             top = fmaxf(top, e[QW - 1]);
-            const bool over = a8_vote(bar, top > (t == 0 ? -INFINITY : A8_OVER));
+            const bool renew = t == 0 || t % A8_RENEW == 2 || raised, over = a8_vote(bar, renew || top > A8_OVER);
+            raised = over && !renew;
             if (t > 0) {   // the output of the tile before: a thread is a dim
                 wait(&ofull, t - 1);
                 tc_fence_after();
@@ -543,36 +556,33 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
 #pragma unroll
                 for (int q = 0; q < QH; ++q) o2[q] = fma2(x[q], down, o2[q]);
             }
-            if (over) {   // new references: the tile's maxima, where they are above
+            if (over) {   // new references: the tile's maxima
 #pragma unroll
                 for (int q = 0; q < QW; ++q) {
                     const float x = a8_warp_max(e[q]);
                     if (lane == 0) s_red[wg][ww][q] = x;
                 }
                 named_sync(bar, 128);
-                float to[QW], corr[QW];
-#pragma unroll
-                for (int q = 0; q < QW; ++q) {
-                    const float x = fmaxf(fmaxf(s_red[wg][0][q], s_red[wg][1][q]), fmaxf(s_red[wg][2][q], s_red[wg][3][q]));
-                    const float m = s_m[q0 + q], ref = -s_nref[q0 + q];
-                    to[q] = fmaxf(m, ref + x);
-                    corr[q] = to[q] == -INFINITY ? 1.f : m == -INFINITY ? 0.f : a8_ex2(m - to[q]);
-                    if (to[q] != -INFINITY) e[q] -= to[q] - ref;
+                if (wt < QW) {   // a thread each; the old references have been read
+                    const int q = q0 + wt;
+                    const float x = fmaxf(fmaxf(s_red[wg][0][wt], s_red[wg][1][wt]), fmaxf(s_red[wg][2][wt], s_red[wg][3][wt]));
+                    const float m = s_m[q], ref = -s_nref[q], r = rintf(ref + x), best = fmaxf(s_best[q], r);
+                    const float to = x == -INFINITY ? m : fmaxf(r, best - A8_DROP);   // the query sees none of the tile's keys
+                    s_corr[q] = to == m ? 1.f : m == -INFINITY ? 0.f : a8_ex2(m - to);
+                    s_by[q] = to == -INFINITY ? 0.f : to - ref;
+                    s_m[q] = to;
+                    s_nref[q] = to == -INFINITY ? 0.f : -to;
+                    s_best[q] = best;
                 }
+                named_sync(bar, 128);
+#pragma unroll
+                for (int q = 0; q < QW; ++q) e[q] -= s_by[q0 + q];
 #pragma unroll
                 for (int q = 0; q < QH; ++q) {
-                    const f2 c = mk2(corr[2 * q], corr[2 * q + 1]);
+                    const f2 c = *(const f2 *)&s_corr[q0 + 2 * q];
                     l2[q] = mul2(l2[q], c);
                     o2[q] = mul2(o2[q], c);
                 }
-                named_sync(bar, 128);   // the old references are read
-#pragma unroll
-                for (int q = 0; q < QW; ++q)
-                    if (wt == q) {
-                        s_m[q0 + q] = to[q];
-                        s_nref[q0 + q] = to[q] == -INFINITY ? 0.f : -to[q];
-                    }
-                named_sync(bar, 128);
             }
             // weights, as planes: column n of key k at group n / 16, then k, then n % 16
             uint8_t *dst = spp + wt * 16;
