@@ -739,7 +739,7 @@ static cudaError_t launch_attn8_h(const Attn8Args &a, int sms, cudaStream_t s) {
     if (a.q_f32) return nq <= 4 ? launch_attn8_t<A8_4F<HD>>(a, sms, s) : launch_attn8_t<A8_8F<HD>>(a, sms, s);
     if (nq <= 4) return launch_attn8_t<A8_4<HD>>(a, sms, s);
     if (nq <= 8) return launch_attn8_t<A8_8<HD>>(a, sms, s);
-    // a rotated bf16 query has more bits than its type: three planes keep 12
+    // a rotated bf16 query has more bits than its type: four planes keep 16, as for fewer queries
     if (nq <= 32) return a.rotate ? launch_attn8_t<A8_16R<HD>>(a, sms, s) : launch_attn8_t<A8_16<HD>>(a, sms, s);
     return a.rotate ? launch_attn8_t<A8_32R<HD>>(a, sms, s) : launch_attn8_t<A8_32<HD>>(a, sms, s);
 }

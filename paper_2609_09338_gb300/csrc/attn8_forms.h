@@ -42,9 +42,9 @@ template <int HD> using A8_4F = A8<HD, 4, 4, 6, 6, 2, 3>;
 template <int HD> using A8_8F = A8<HD, 8, 8, 6, 6, 2, 2>;
 template <int HD> using A8_4 = A8<HD, 4, 4, 4, 4, 2, 3>;
 template <int HD> using A8_8 = A8<HD, 8, 8, 4, 4, 2, 3>;
-template <int HD> using A8_16R = A8<HD, 16, 8, 3, 4, 2, 2>;
+template <int HD> using A8_16R = A8<HD, 16, 8, 4, 4, 2, 2>;
 template <int HD> using A8_16 = A8<HD, 16, 8, 2, 4, 2, 3>;
-template <int HD> using A8_32R = A8<HD, 32, 8, 3, 4, 1, 4>;
+template <int HD> using A8_32R = A8<HD, 32, 8, 4, 4, 1, 4>;
 template <int HD> using A8_32 = A8<HD, 32, 8, 2, 4, 1, 4>;
 
 }  // namespace osp
