@@ -222,8 +222,8 @@ int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, in
  * as 2^-40 of the row's largest at least: the weights behind a key that takes nearly all
  * of a row's keep their bits, whatever their share.  No workspace.
  * Device errors: INVALID_ARG (n_rows[b] outside 0 .. max_rows, or more than T),
- * CAPACITY (T past the page table, a page id out of range); such a sequence's
- * output rows are 0.
+ * CAPACITY (T past the page table, a finished page's id out of range); all output rows
+ * of such a sequence are 0 (a negative count has none).
  * Host errors: INVALID_ARG, DTYPE. */
 int osprey_kv8_attend(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, int B, int max_rows,
                       const int32_t *n_rows, const void *q, int dtype, int64_t q_stride, int rotate, int advanced,

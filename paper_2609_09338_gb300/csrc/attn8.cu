@@ -314,6 +314,11 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
         }
         scales(0);
         ids = key_id(1);
+        // A bad id clears all rows of its sequence, so pages that this tile's rows do not see are checked too.
+        // (A draft call's first kernel has checked them.)
+        if (a.seq_len)
+            for (int p = np_all + rank * C::CT + tid; p < c8; p += cs * C::CT)
+                block_of(__ldcg(a.page_table + (size_t)b * a.max_pages + p));
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             const int q = warp + u * W_MMA, j = (i0 + q) >> lg;
