@@ -215,8 +215,9 @@ int osprey_kv8_append(const osprey_ctx *ctx, const osprey_kv8 *kv, int layer, in
  *   out [B][max_rows][n_q_heads][head_dim] of q's type, 16-byte aligned; rows from
  *          n_rows[b] on are left as they were
  * Sums and softmax statistics are float32; q and the weights enter the tensor
- * cores as e4m3 planes: bf16 queries exactly (rotated ones to 16 significant bits),
- * float32 queries to 24.  A weight is off by at most 2^-16 of itself (float32
+ * cores as e4m3 planes.  bf16 queries do so exactly, rotated ones with 16 significant
+ * bits, float32 ones with 24; elements under 2^-13 of their row's largest are within
+ * 2^-21 (2^-29, 2^-37) of that.  A weight is off by at most 2^-16 of itself (float32
  * queries: 2^-24) or, if that is more, 2^-25 (2^-33) of the largest one that its row has
  * in the 17 x 128 keys up to its own (each weight times its block's v_scale), which counts
  * as 2^-40 of the row's largest at least: the weights behind a key that takes nearly all

@@ -13,8 +13,9 @@
 // wide comes as e4m3 planes, the operand's other side: x 2^e = x0 + x1/16 + x2/256 ...,
 // each plane the nearest e4m3 (4 significant bits) of 16 times what the one before it
 // left.  Planes have columns of their own (N = planes x queries) and are put together in
-// float32, so no product of unlike sizes shares an accumulator.  bf16 queries are two
-// planes exactly.
+// float32, so no product of unlike sizes shares an accumulator.  A bf16 query, scaled to
+// a magnitude of 128 to 256, is two planes: exactly where an element is 2^-13 of its row's
+// largest or more, within 2^-21 of the largest elsewhere (two planes end at 2^-13).
 //
 // Per tile of 128 keys a thread is a key: it reads its scores from TMEM and writes its
 // weights' planes; then it is a dim, and adds the output of the tile before from TMEM to
@@ -195,7 +196,9 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     bool ok = true;
     if (a.seq_len) {
         // Everything that this call reads may come from the kernel before, which this one may
-        // have started beside: it is read through L2, and by the copies after a proxy fence.
+        // have started beside: nothing is read before this wait, which makes that kernel's
+        // writes visible to plain loads, and to the copies behind a proxy fence.  (Queries and
+        // the tail through L2 alone: groups of rows 171 -> 182 us, 206 -> 214.)
         pdl_wait();
         asm volatile("fence.proxy.async.global;" ::: "memory");
         nr = __ldcg(a.n_rows + b);
