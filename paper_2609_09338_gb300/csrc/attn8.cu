@@ -176,14 +176,14 @@ __device__ __forceinline__ bool a8_wait(uint64_t *bar, uint32_t parity, int *abo
 
 template <typename C>
 __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_constant__ Attn8Args a, int tiles) {
-    constexpr int HD = C::HD, QT = C::QT, QW = C::QW, QP = C::QP, PP = C::PP, KB = C::KB, TB = C::TB, NS = C::NS, NSB = C::NSB;
+    constexpr int HD = C::HD, QT = C::QT, QW = C::QW, QP = C::QP, PP = C::PP, KB = C::KB, TB = C::TB, NS = C::NS;
     constexpr int W_MMA = C::CT / 32, W_K = W_MMA + 1;   // the warps that do not compute: products, K copies, V copies
     extern __shared__ __align__(1024) uint8_t sm[];
     uint8_t *sk = sm, *sv = sk + NS * TB, *sqp = sv + NS * TB, *spp = sqp + C::QB;
     float *sq = (float *)spp;                       // [QT][HD] while the tail is read
     float *sp = (float *)(spp + C::PB);             // [QT][A8_CH] the tail's weights
     float *so = (float *)sk;                        // [QT][HD] at the end
-    __shared__ __align__(8) uint64_t kfull[NS], vfull[NS], kfree[NS], vfree[NS], sfull[2], sread[1], pready, ofull;
+    __shared__ __align__(8) uint64_t kfull[NS], vfull[NS], kfree[NS], vfree[NS], sfull[2], pready, ofull;
     __shared__ __align__(16) float s_red[C::NWG][4][QW], s_mul[QT], s_nref[QT], s_m[QT], s_best[QT], s_corr[QT], s_by[QT];
     __shared__ float s_l[QT], s_lw[4][QT];
     __shared__ int s_pos[QT], s_bad, s_abort;
@@ -258,7 +258,6 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
         if (lane == 0) {
             mbar_init(&sfull[0], 1);
             mbar_init(&sfull[1], 1);
-            mbar_init(sread, 4 * nact);
             mbar_init(&ofull, 1);
             mbar_init(&pready, 4 * nact);
             s_bad = !ok;
@@ -375,7 +374,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     tc_fence_after();
     // not before this block holds its TMEM: a dependent's blocks take theirs and wait for this kernel
     pdl_trigger();
-    const uint32_t tmem = s_tmem, tm_o = tmem + NSB * C::SC;
+    const uint32_t tmem = s_tmem, tm_o = tmem + 2 * C::SC;
     // After a wait that ran out nothing is waited for or issued any more: the loops run to
     // their ends, and the cluster's outputs are 0.
     auto wait1 = [&](uint64_t *bar, uint32_t phase) { return a8_wait(bar, phase & 1, &s_abort, a.status); };
@@ -393,10 +392,9 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
             const uint64_t dV = a8_desc(smem_u32(sv), KB, 128), dP = a8_desc(smem_u32(spp), 128, A8_PG);
             int ks = 0, kph = 0, vs = 0, vph = 0;   // slots and their phases
             auto scores = [&](int t) {   // of tile t: 128 keys x (planes x queries)
-                const int sb = NSB == 2 ? t & 1 : 0;
+                const int sb = t & 1;
                 if (!wait1(&kfull[ks], kph)) return false;
-                // the columns' last readers have read them (two score buffers: before the weights of tile t - 2 were written)
-                if (NSB == 1 && t > 0 && !wait1(sread, t - 1)) return false;
+                // the columns' last readers had read them before they wrote the weights of tile t - 2
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < HD / 32; ++k)
@@ -528,12 +526,9 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
                 lvs = lvs < A8_LO ? A8_LO : lvs;
             }
             f2 e2[QH];   // log2 of the weights
-            wait(&sfull[t % NSB], t / NSB);
+            wait(&sfull[t & 1], t >> 1);
             tc_fence_after();
-            a8_planes<QT, QW, QP>(tmem + lanes + t % NSB * C::SC + q0, e2);
-            tc_fence_before();
-            __syncwarp();
-            if (NSB == 1 && lane == 0) mbar_arrive(sread);
+            a8_planes<QT, QW, QP>(tmem + lanes + (t & 1) * C::SC + q0, e2);
             const f2 ks2 = mk2(ks, ks), lv2 = mk2(lvs, lvs);
             float e[QW];
 #pragma unroll

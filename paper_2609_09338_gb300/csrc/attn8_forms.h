@@ -18,8 +18,7 @@ struct A8 {
     static constexpr int KB = 16 * HD, TB = 8 * KB;       // bytes of a page, of a tile's slot
     static constexpr int SC = (QP * QT + 15) / 16 * 16, OC = (PP * QT + 15) / 16 * 16;   // TMEM columns of scores, output
     static constexpr int TM = 512 / BPS;                  // columns a block may take
-    static constexpr int NSB = 2 * SC + OC <= TM ? 2 : 1;
-    static constexpr int USED = NSB * SC + OC;
+    static constexpr int USED = 2 * SC + OC;               // two tiles' scores, one's output
     static constexpr int COLS = USED <= 32 ? 32 : USED <= 64 ? 64 : USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
     static constexpr int QB = SC * HD;                    // bytes of q's planes
     static constexpr int PW = A8_PG * (OC / 16);          // bytes of the weights' planes
