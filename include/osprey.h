@@ -185,7 +185,12 @@ int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv, int layer,
  *   page_table, seq_len, max_pages_per_seq, n_pages as osprey_kv
  *   tail_pages >= 1.  A caller may take back the last 16 * (tail_pages - 1)
  *           positions of a sequence by lowering seq_len (or by not advancing it):
- *           the rows of the page that is unfinished then are still in the tail. */
+ *           the rows of the page that is unfinished then are still in the tail.
+ *           They count from the last row written, committed or not: after
+ *           osprey_draft_step_kv8, whose chain writes K - 1 rows behind the
+ *           committed ones, 16 * (tail_pages - 1) - (K - 1) positions of seq_len
+ *           can be taken back.  Further back the tail holds later rows' values,
+ *           which no call can tell. */
 typedef struct osprey_kv8 {
     void *k8, *v8;
     float *k_scale, *v_scale;
@@ -265,7 +270,8 @@ int osprey_draft_step(osprey_ctx *ctx, const osprey_kv *kv, int B, int K, int ma
  * bf16 cache rounds them; at the call's end the pages that the committed rows
  * finish are rounded to 8 bits.  Verification stays lossless: it divides by the
  * q that the tokens were drawn from.
- *   kv: tail_pages with 16 * tail_pages >= 14 + max_new + K (CAPACITY)
+ *   kv: tail_pages with 16 * tail_pages >= 14 + max_new + K (CAPACITY); more of them
+ *          where positions are to be taken back behind the call (osprey_kv8)
  *   workspace: osprey_draft_kv8_workspace_bytes
  * Everything else as osprey_draft_step; B <= 4096. */
 size_t osprey_draft_kv8_workspace_bytes(const osprey_ctx *ctx, int B, int K, int max_new, int max_pages_per_seq);

@@ -13,7 +13,8 @@
 //   K (the reduction runs over dims):   [slot / 8][dim / 16][slot % 8][dim % 16]
 //   V (the reduction runs over slots):  [dim][slot]
 // Rows of the unfinished page stay in bf16 in the tail, a ring of tail_pages pages
-// a sequence that always holds the last rows appended: each value is rounded to 8
+// a sequence that always holds the last rows written (a draft call's chain's rows, which
+// nobody has committed, take the place of older ones too): each value is rounded to 8
 // bits once, with its block's final scale, however many calls append the block.
 #pragma once
 
