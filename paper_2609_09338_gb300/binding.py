@@ -231,6 +231,18 @@ class KvCache:
     page_table: torch.Tensor   # [B, max_pages] int32
     seq_len: torch.Tensor      # [B] int32
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_device", None)
+
+    @property
+    def device(self) -> int:
+        """The CUDA device of all four tensors; -1: none, or not the same."""
+        if self._device is None:
+            d = {t.get_device() for t in (self.k_pages, self.v_pages, self.page_table, self.seq_len)}
+            object.__setattr__(self, "_device", d.pop() if len(d) == 1 else -1)
+        return self._device
+
     @property
     def max_pages(self) -> int:
         return self.page_table.shape[1]
@@ -282,12 +294,12 @@ class Kv8Cache:
         return self.k_tail.shape[1] // max(1, self.page_table.shape[0])
 
     def c_struct(self, shape: DrafterShape) -> osprey_kv8:
-        """The C struct.  The tensors are checked against the drafter's shape when one of them, or the batch, is
-        another than at the check before."""
+        """The C struct.  The tensors are checked against the drafter's shape and the current device when one of them,
+        the batch or the device is another than at the check before."""
         k8, v8, ks, vs, kt, vt = self.k8, self.v8, self.k_scale, self.v_scale, self.k_tail, self.v_tail
         tab, n = self.page_table, self.seq_len
-        checked = self._checked
-        if checked is None or checked[0] is not shape or checked[1] != tab.shape:
+        checked, device = self._checked, torch._C._cuda_getDevice()
+        if checked is None or checked[0] is not shape or checked[1] != tab.shape or checked[2] != device:
             L, H, hd = shape.n_layers, shape.n_kv_heads, shape.head_dim
             _need(tab, torch.int32, None, "page_table")
             if tab.dim() != 2 or k8.dim() != 4:
@@ -300,10 +312,12 @@ class Kv8Cache:
             _need(kt, torch.bfloat16, (L, B * t, H, 16, hd), "k_tail")
             _need(vt, torch.bfloat16, (L, B * t, H, 16, hd), "v_tail")
             _need(n, torch.int32, (B,), "seq_len")
-            checked = (shape, tab.shape, tab.shape[1], pages, t)
+            if any(x.get_device() != device for x in (k8, v8, ks, vs, kt, vt, tab, n)):
+                _elsewhere(device)
+            checked = (shape, tab.shape, device, tab.shape[1], pages, t)
             object.__setattr__(self, "_checked", checked)
         return osprey_kv8(k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), kt.data_ptr(), vt.data_ptr(),
-                          tab.data_ptr(), n.data_ptr(), *checked[2:])
+                          tab.data_ptr(), n.data_ptr(), *checked[3:])
 
 
 def alloc_kv8(shape: DrafterShape, page_table: np.ndarray, n_pages: int, tail_pages: int = 2, device="cuda") -> Kv8Cache:
@@ -351,6 +365,10 @@ def osprey_kv_append(ctx: Ctx, kv: KvCache, n_rows: torch.Tensor, k_rows: torch.
 _ROWS = {torch.bfloat16: OSPREY_BF16, torch.float32: OSPREY_F32}
 
 
+def _elsewhere(d):
+    raise ValueError(f"every tensor must be on the current device, {d}")
+
+
 def _strided_rows(t, lead, inner, name):
     """Checks rows [*lead, *inner] whose last two dimensions are dense; the distance between rows, in elements."""
     if t.dtype not in _ROWS:
@@ -375,8 +393,11 @@ def _strided_rows(t, lead, inner, name):
 
 def _append_rows(ctx, B, n_rows, k_rows, v_rows, status, layer):
     s = ctx.shape
-    _need(n_rows, torch.int32, (B,), "n_rows")
-    _need(status, torch.int32, (1,), "status")
+    _need(n_rows, torch.int32, (B,), "n_rows", False)
+    _need(status, torch.int32, (1,), "status", False)
+    d = torch._C._cuda_getDevice()
+    if n_rows.get_device() != d or status.get_device() != d:
+        _elsewhere(d)
     lead = tuple(k_rows.shape[:-2])
     if len(lead) != (2 if layer is None else 1):
         raise ValueError("rows are [n_layers, total, Hkv, hd], or [total, Hkv, hd] of one layer")
@@ -396,6 +417,8 @@ def osprey_kv_append_rope(ctx: Ctx, kv: KvCache, n_rows: torch.Tensor, k_rows: t
     float32; rows may be views into a wider projection's output."""
     B = kv.page_table.shape[0]
     total, stride = _append_rows(ctx, B, n_rows, k_rows, v_rows, status, layer)
+    if kv.device != torch._C._cuda_getDevice():
+        _elsewhere(torch._C._cuda_getDevice())
     kvs = kv.c_struct()
     _check(_c_kv_append_rope(ctx.handle, ctypes.byref(kvs), -1 if layer is None else layer, B, _ptr(n_rows), total,
                              _ptr(k_rows), _ptr(v_rows), _ROWS[k_rows.dtype], stride, int(advance), _ptr(status),
@@ -424,9 +447,12 @@ def osprey_kv8_attend(ctx: Ctx, kv: Kv8Cache, layer: int, n_rows: torch.Tensor, 
         raise ValueError("q is [B, max_rows, Hq, hd]")
     R = q.shape[1]
     stride = _strided_rows(q, (B, R), (s.n_q_heads, s.head_dim), "q")
-    _need(n_rows, torch.int32, (B,), "n_rows")
-    _need(out, q.dtype, (B, R, s.n_q_heads, s.head_dim), "out")
-    _need(status, torch.int32, (1,), "status")
+    _need(n_rows, torch.int32, (B,), "n_rows", False)
+    _need(out, q.dtype, (B, R, s.n_q_heads, s.head_dim), "out", False)
+    _need(status, torch.int32, (1,), "status", False)
+    d = torch._C._cuda_getDevice()
+    if n_rows.get_device() != d or out.get_device() != d or status.get_device() != d:
+        _elsewhere(d)
     kvs = kv.c_struct(s)
     _check(_c_kv8_attend(ctx.handle, ctypes.byref(kvs), layer, B, R, _ptr(n_rows), _ptr(q), _ROWS[q.dtype], stride,
                          int(rotate), int(advanced), _ptr(out), _ptr(status), _stream(stream)))
