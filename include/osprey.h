@@ -179,7 +179,8 @@ int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv, int layer,
  *           smallest power of two, at least 2^-100, with max |x| <= 448 scale; NaN
  *           (and codes 0) for a block with a value that is not finite, so that
  *           every output that sees a key of the block is NaN.  Attention takes any
- *           positive scale, V's up to 2^40.
+ *           positive scale, V's up to 2^40; what a block of V scale under 2^-60 gives
+ *           to an output is right to 2^-70, not relative to itself.
  *   k_tail, v_tail [n_layers][B][tail_pages][n_kv_heads][16][head_dim] bf16:
  *           position t of sequence b in ring page (t / 16) % tail_pages, slot t % 16
  *   page_table, seq_len, max_pages_per_seq, n_pages as osprey_kv

@@ -57,7 +57,10 @@ namespace osp {
 
 namespace cg = cooperative_groups;
 
-constexpr float A8_LO = -40.f;       // smallest log2 of a V scale that moves the reference
+// Smallest log2 of a V scale that moves the reference.  Lower, and the sum of the weights (up to
+// 2^(A8_OVER - A8_LO + A8_DROP) a key) or a weight beside one of V scale 2^40 would leave
+// float32's range; the values of such a block have steps of 2^(A8_LO - 25) in the output.
+constexpr float A8_LO = -60.f;
 constexpr float A8_OVER = 4.f;       // a weight is at most 2^A8_OVER, times A8_UP an e4m3 number
 constexpr float A8_DROP = 40.f;      // a reference is at least 2^-A8_DROP of the largest one so far
 constexpr int A8_RENEW = 16;         // tiles a reference stays at most
@@ -521,8 +524,8 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
             asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rvs) : "f"(vs));
             float fvs = A8_UP;
             if (!(lvs >= A8_LO)) {
-                fvs = lvs < A8_LO ? vs * 0x1p40f * A8_UP : A8_UP;
-                rvs = lvs < A8_LO ? 0x1p40f : 1.f;
+                fvs = lvs < A8_LO ? vs * 0x1p60f * A8_UP : A8_UP;
+                rvs = lvs < A8_LO ? 0x1p60f : 1.f;
                 lvs = lvs < A8_LO ? A8_LO : lvs;
             }
             f2 e2[QH];   // log2 of the weights
