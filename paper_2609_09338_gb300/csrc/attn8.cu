@@ -36,13 +36,14 @@
 //
 // Measured (GB300, keys of 8 KV heads of 128).  One row of 64 sequences of 1024..16384
 // keys: 174 us, 6.55 TB/s, bound by memory (0.97 of a plain copy's rate).  Groups of four,
-// 1..8 rows of 96 sequences of 1024..4096 keys: 173 us; 50..64 rows of 8 sequences of
+// 1..8 rows of 96 sequences of 1024..4096 keys: 172 us; 50..64 rows of 8 sequences of
 // 2000..8192 keys: 206 us (160 and 190 with three planes of the weights, 12 bits instead of
-// 16); these are bound by the arithmetic between the two products and by a tile's chain.
+// 16).  Both wait for a tile's chain, scores to weights to outputs: half of the issue slots
+// are used, 375 instructions a warp and tile, 15 % of the tensor pipe.
 // float32 queries, groups of four, 16 sequences of 2048..8192 keys of 4 heads: 26 us.  A
-// call of one sequence takes 6.5 us.  Taking sequences longest first (a ranking in each
-// block) made the first 183 us, the second 163, and the third, which is 187 to 207 with
-// the sequences' order, 189: sequences are taken as they come.
+// call of one sequence takes 6.3 us.  Taking sequences longest first (a ranking in each
+// block) made the first 183 us, and with three planes the second 163, the third, which was
+// 187 to 207 with the sequences' order, 189: sequences are taken as they come.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -735,10 +736,10 @@ static cudaError_t launch_attn8_t(const Attn8Args &a, int sms, cudaStream_t s) {
 // heads of a group), up to 8 with two blocks an SM.  More go 16 at a time, two blocks an
 // SM, up to 32 of them, else 32 at a time: a block of 32 has the SM to itself.  Numbers of
 // rows mostly differ from sequence to sequence, and blocks of 16 leave fewer warps idle
-// where they do.  us a call, 16 / 32 at a time: 1..8 rows of 96 sequences, groups of four
-// 160 / 183; 1..16 rows of 64, groups of two 77 / 91; 8 rows of each of 32 sequences,
-// groups of four 93 / 83, 4 rows 51 / 68, 16 rows 162 / 157; 50..64 rows of 8 205 / 187.
-// Float32 queries take twice the planes.
+// where they do.  us a call, 16 / 32 at a time, 1024..4096 keys: 1..8 rows of 96 sequences,
+// groups of four 171 / 193; 1..16 rows of 64, groups of two 121 / 133; 4, 8 and 16 rows of
+// each of 32 sequences, groups of four 59 / 75, 88 / 89 and 141 / 135; 50..64 rows of 8
+// sequences of 2000..8192 keys 226 / 206; four prompts of 2048 rows 967 / 918.
 template <int HD>
 static cudaError_t launch_attn8_h(const Attn8Args &a, int sms, cudaStream_t s) {
     const int nq = a.max_rows * (a.Hq / a.Hkv);

@@ -198,9 +198,10 @@ constexpr int kr_blocks = RF32 ? (HD == 128 ? 3 : 4) : 5;
 //
 // 33 k rows of 16 sequences, two layers of 4 heads of 128, with the lengths' update: to the
 // bf16 cache 50 us, 5.5 TB/s, bound by memory (0.82 of a plain copy's rate); to the 8-bit
-// one 42 us, 4.9 TB/s (0.72), bound by its instructions (some 900 a 4 KB block: unpack,
-// turn, round, maximum, scale, round) and the barriers between pages.  A decode step (one row of 64 sequences) takes 4.2
-// and 5.4 us: the chain of lengths, page, rows and angles.
+// one 42 us, 4.9 TB/s (0.72): some 900 instructions a 4 KB block (unpack, turn, round,
+// maximum, scale, round) take 53 % of the issue slots, and the four warps meet three times
+// a page.  A decode step (one row of 64 sequences) takes 4.2 and 5.4 us: the chain of
+// lengths, page, rows and angles.
 template <int HD, bool EIGHT, bool RF32>
 __global__ void __launch_bounds__(KR_THREADS, (kr_blocks<HD, RF32>)) kv_rope_kernel(const __grid_constant__ KvRopeArgs a) {
     __shared__ int64_t sh[KR_WARPS][2];

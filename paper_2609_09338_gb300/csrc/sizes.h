@@ -146,9 +146,11 @@ inline int tree_cluster(int B, double row_kb, bool greedy, const bool (&cached)[
 // and store beside its share of the keys; units that do not all fit at once
 // (`at_once` blocks) take their mean share of the device and end with a whole one, and
 // are half as long as the longest on average.  us a call with clusters of 1, 2, 4 and 8
-// (the chosen one first): 512 units of 1024..16384 keys 2: 174 (191, 192, 259); 64 of
-// 2048..8192 4: 27 (53, 34, 37); 8 of 2048 8: 7.2 (15.2, 10.7, 8.3); 768 of up to 32
-// queries, 1024..4096 keys 1: 190 (262, 429, 886).
+// (the chosen one first): 512 units of 1024..16384 keys 2: 175 (190, 191, 255); 64 of
+// 2048..8192 4: 26 (51, 33, 36); 8 of 2048 8: 6.6 (14.8, 10.3, 7.9); 1536 of up to 16
+// queries, 1024..4096 keys 1: 171 (219, 323, 542).  `tiles` are the page table's: the host
+// does not know the lengths, and a table far wider than they are makes the clusters larger
+// than these.
 inline int attn8_split(long long units, long long at_once, int tiles) {
     int pick = 1;
     double best = 0;
