@@ -6,7 +6,7 @@ namespace osp {
 constexpr int A8_CH = 32;            // tail keys of a step
 constexpr int A8_PG = 2048;          // bytes of 16 weight columns of a tile
 constexpr int A8_SM = 228 * 1024;    // shared memory of an SM; a block takes 1 KB beside its own
-constexpr int A8_OPT = 227 * 1024;   // of one block, at most
+constexpr int A8_OPT = 227 * 1024;   // of one block, at most, 3 KB of static arrays among it
 
 // QT queries a block, QW of them a warpgroup's (4 warps); QP and PP planes of a query and
 // of a weight; BPS blocks an SM, of NS slots of K and V each.
@@ -31,7 +31,7 @@ struct A8 {
     // blocks of 256 columns fit or one of 512, and no other beside it.
     static constexpr int SHARE = A8_SM / 3 * (BPS == 2 ? 1 : 2);
     static constexpr int SMEM = NEED > SHARE ? NEED : SHARE;
-    static_assert(BPS == 1 || BPS == 2, "shares are thirds");
+    static_assert((BPS == 1 || BPS == 2) && SMEM + 3 * 1024 <= A8_OPT, "shares are thirds");
     static_assert((QW == 4 || QW == 8) && COLS <= TM && QB + PB >= KB && QT % QW == 0, "operands");
     static_assert(QT * HD * 4 <= NS * TB, "the merge's outputs take the K slots");
 };
