@@ -83,6 +83,13 @@ __device__ __forceinline__ void a8_mma(uint32_t d, uint64_t a, uint64_t b, uint3
                  "l"(a), "l"(b), "r"(idesc), "r"(acc)
                  : "memory");
 }
+__device__ __forceinline__ void a8_alloc(uint32_t *at, int columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(at)), "r"((uint32_t)columns)
+                 : "memory");
+}
+__device__ __forceinline__ void a8_dealloc(uint32_t at, int columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"((uint32_t)columns) : "memory");
+}
 __device__ __forceinline__ float a8_ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -191,7 +198,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     __shared__ __align__(16) float s_red[C::NWG][4][QW], s_mul[QT], s_nref[QT], s_m[QT], s_best[QT], s_corr[QT], s_by[QT];
     __shared__ float s_l[QT], s_lw[4][QT];
     __shared__ int s_pos[QT], s_bad, s_abort;
-    __shared__ uint32_t s_tmem;
+    __shared__ uint32_t s_tmem[2];
     cg::cluster_group cluster = cg::this_cluster();
     const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int unit = blockIdx.x / cs, kvh = unit % a.Hkv, tile = unit / a.Hkv % tiles, b = unit / a.Hkv / tiles;
@@ -269,8 +276,8 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
             mbar_fence_init();
         }
         __syncwarp();
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)),
-                     "r"((uint32_t)C::COLS));
+        a8_alloc(&s_tmem[0], C::SCOLS);
+        a8_alloc(&s_tmem[1], C::OCOLS);
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     } else if (warp >= W_K) {
         int first[NS];
@@ -378,7 +385,7 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     tc_fence_after();
     // not before this block holds its TMEM: a dependent's blocks take theirs and wait for this kernel
     pdl_trigger();
-    const uint32_t tmem = s_tmem, tm_o = tmem + 2 * C::SC;
+    const uint32_t tmem = s_tmem[0], tm_o = s_tmem[1];
     // After a wait that ran out nothing is waited for or issued any more: the loops run to
     // their ends, and the cluster's outputs are 0.
     auto wait1 = [&](uint64_t *bar, uint32_t phase) { return a8_wait(bar, phase & 1, &s_abort, a.status); };
@@ -676,7 +683,8 @@ __global__ void __launch_bounds__(C::THREADS, C::BPS) attn8_kernel(const __grid_
     else __syncthreads();
     if (warp == W_MMA) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::COLS));
+        a8_dealloc(tmem, C::SCOLS);
+        a8_dealloc(tm_o, C::OCOLS);
     } else if (warp < W_MMA) {
         // lane r holds what rank r left of a query; a thread is a dim of the output
         if (cs == 1 && wt < HD && warp < 4 * nact) {

@@ -5,8 +5,13 @@ namespace osp {
 
 constexpr int A8_CH = 32;            // tail keys of a step
 constexpr int A8_PG = 2048;          // bytes of 16 weight columns of a tile
-constexpr int A8_SM = 228 * 1024;    // shared memory of an SM; a block takes 1 KB beside its own
-constexpr int A8_OPT = 227 * 1024;   // of one block, at most, 3 KB of static arrays among it
+constexpr int A8_SM = 228 * 1024;    // shared memory of an SM,
+constexpr int A8_OPT = 227 * 1024;   // of one block at most,
+constexpr int A8_OWN = 1024;         // of a block beside what it asks for,
+constexpr int A8_STATIC = 3 * 1024;  // of its static arrays, at most
+
+// Columns of an allocation: a power of two, 32 or more.
+constexpr int a8_columns(int n) { return n <= 32 ? 32 : 2 * a8_columns((n + 1) / 2); }
 
 // QT queries a block, QW of them a warpgroup's (4 warps); QP and PP planes of a query and
 // of a weight; BPS blocks an SM, of NS slots of K and V each.
@@ -17,22 +22,28 @@ struct A8 {
     static constexpr int THREADS = CT + 96;               // and three warps: products, K copies, V copies
     static constexpr int KB = 16 * HD, TB = 8 * KB;       // bytes of a page, of a tile's slot
     static constexpr int SC = (QP * QT + 15) / 16 * 16, OC = (PP * QT + 15) / 16 * 16;   // TMEM columns of scores, output
-    static constexpr int TM = 512 / BPS;                  // columns a block may take
-    static constexpr int USED = 2 * SC + OC;               // two tiles' scores, one's output
-    static constexpr int COLS = USED <= 32 ? 32 : USED <= 64 ? 64 : USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
+    // TMEM, in two pieces: two tiles' scores, one's output
+    static constexpr int SCOLS = a8_columns(2 * SC), OCOLS = a8_columns(OC);
     static constexpr int QB = SC * HD;                    // bytes of q's planes
     static constexpr int PW = A8_PG * (OC / 16);          // bytes of the weights' planes
     static constexpr int PB = PW > QT * HD * 4 ? PW : QT * HD * 4;   // their place, q's for the tail
     static constexpr int NEED = 2 * NS * TB + QB + PB + QT * A8_CH * 4;
-    // A block waits for its TMEM columns without a limit, and its cluster waits for it: were
-    // there more blocks on an SM than its columns serve, of one call or of two, each could
-    // hold what the other's cluster waits for.  So a block asks for at least a third of the
-    // SM's shared memory, with the SM to itself two thirds: whatever the forms, either two
-    // blocks of 256 columns fit or one of 512, and no other beside it.
-    static constexpr int SHARE = A8_SM / 3 * (BPS == 2 ? 1 : 2);
+    // A block waits for its TMEM without a limit, and its cluster waits for it, so it may never
+    // wait for a block that a cluster of this kernel, of this call or of another stream's, waits
+    // with.  Two things see to that, whatever the compiler's register counts are:
+    // - Two blocks of these forms (one, where BPS is 1) take all of an SM's shared memory: beside
+    //   them is no third, and no other kernel's block that holds or queues for TMEM.
+    // - Two blocks' pieces fit wherever the first ones lie.  Nothing says that an allocation is
+    //   aligned, and a block that has left may have pushed one to any column: of 16 units of 32
+    //   columns, pieces of 4 and 2 leave 10 in three gaps, one of them of 4 at least, and then 6
+    //   in four gaps, one of them of 2.  (One piece of 8 units in the middle would leave two gaps of 4.)
+    // What else a block may meet on its SM ends by itself: it holds its TMEM before it lets a
+    // dependent start, and waits for none of these blocks unless all of those hold theirs.
+    static constexpr int SHARE = (A8_SM / BPS < A8_OPT + A8_OWN ? A8_SM / BPS : A8_OPT + A8_OWN) - A8_OWN - A8_STATIC;
     static constexpr int SMEM = NEED > SHARE ? NEED : SHARE;
-    static_assert((BPS == 1 || BPS == 2) && SMEM + 3 * 1024 <= A8_OPT, "shares are thirds");
-    static_assert((QW == 4 || QW == 8) && COLS <= TM && QB + PB >= KB && QT % QW == 0, "operands");
+    static_assert(SMEM + A8_STATIC <= A8_OPT && BPS * (SMEM + A8_STATIC + A8_OWN) <= A8_SM, "shared memory");
+    static_assert(BPS == 1 ? SCOLS + OCOLS <= 512 : BPS == 2 && SCOLS <= 128 && OCOLS <= 64, "TMEM");
+    static_assert((QW == 4 || QW == 8) && QB + PB >= KB && QT % QW == 0, "operands");
     static_assert(QT * HD * 4 <= NS * TB, "the merge's outputs take the K slots");
 };
 
