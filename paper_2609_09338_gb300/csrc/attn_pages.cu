@@ -50,6 +50,7 @@ constexpr int AP_COST_PAIR = 4, AP_COST = 1;
 __host__ __device__ constexpr int ap_cost(bool lists, bool pair) { return lists ? 0 : pair ? AP_COST_PAIR : AP_COST; }
 constexpr int AP_BLOCKS = 4;          // blocks that plan: each counts everything and writes its share of the units
 constexpr int AP_PLAN = 1024;         // threads of the planning block
+constexpr int AP_MAXB = 4096;
 constexpr int AP_SHARE = 128;         // a prefix is shared where a sequence has fewer queries a KV head
 
 template <int HD_, bool F32_>
@@ -229,24 +230,46 @@ __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs
     int *s_punit = s_cnt + B, *s_ptile = s_punit + B, *s_unit = s_ptile + B, *s_tile = s_unit + B;
     __shared__ unsigned long long sh[32][4];
     __shared__ int s_bad, s_split;
+    __shared__ uint32_t s_begin[AP_MAXB / 32];   // a bit a sequence
     const int nb = (int)gridDim.x, rank = (int)blockIdx.x;
     if (tid == 0) s_bad = s_split = 0;
     for (int b = tid; b < B; b += AP_PLAN) s_cnt[b] = 0;
     pdl_wait();
     pdl_trigger();
     const bool lists = a.pages != nullptr, split = a.share && (a.max_rows << lg) < AP_SHARE;
-    for (int b = tid; b < B; b += AP_PLAN) {
-        const SeqRows r = seq_rows(a.n_rows[b], a.seq_len[b], a.advanced, a.max_rows, a.max_pages);
-        s_n[b] = r.code ? -1 : r.n;
-        s_base[b] = r.base;
-        const int s = a.share ? a.share[b] : -1;
-        s_lead[b] = s == -1 ? b : s;
-        s_pre[b] = a.share ? a.shared_len[b] : 0;
-        if (rank == 0) w.bad[b] = r.code != 0;
-        if (rank == 0) w.bad_pre[b] = 0;
-        if (r.code && rank == 0) set_status(a.status, r.code);
+    for (int b0 = 0; b0 < B; b0 += AP_PLAN) {
+        const int b = b0 + tid;
+        bool begins = false;   // a run, or none of them: its first sequence is not the one before's
+        if (b < B) {
+            const SeqRows r = seq_rows(a.n_rows[b], a.seq_len[b], a.advanced, a.max_rows, a.max_pages);
+            s_n[b] = r.code ? -1 : r.n;
+            s_base[b] = r.base;
+            auto first = [&](int x) {
+                const int s = a.share ? a.share[x] : -1;
+                return s == -1 ? x : s;
+            };
+            const int lead = first(b);
+            begins = b == 0 || lead == b || lead != first(b - 1);
+            s_lead[b] = lead;
+            s_pre[b] = a.share ? a.shared_len[b] : 0;
+            if (rank == 0) w.bad[b] = r.code != 0;
+            if (rank == 0) w.bad_pre[b] = 0;
+            if (r.code && rank == 0) set_status(a.status, r.code);
+        }
+        const uint32_t mask = __ballot_sync(0xffffffffu, begins);
+        if (lane == 0) s_begin[b0 / 32 + warp] = mask;
     }
     __syncthreads();
+    // no run begins in lead + 1 .. b: all of them, and lead itself, say that lead is their first
+    auto together = [&](int lead, int b) {
+        for (int i = (lead + 1) / 32; i <= b / 32; ++i) {
+            uint32_t m = s_begin[i];
+            if (i == (lead + 1) / 32) m &= ~0u << ((lead + 1) & 31);
+            if (i == b / 32) m &= ~0u >> (31 - (b & 31));
+            if (m) return false;
+        }
+        return true;
+    };
     // runs: checked against what the sequences said, then written over it
     unsigned long long rows = 0;
     for (int b0 = 0; b0 < B; b0 += AP_PLAN) {
@@ -258,7 +281,7 @@ __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs
             lead = s_lead[b];
             bool ok = n >= 0;
             if (a.share) {
-                const bool run = lead == b || (lead >= 0 && lead < b && s_lead[b - 1] == lead && s_lead[lead] == lead);
+                const bool run = lead == b || (lead >= 0 && lead < b && together(lead, b));
                 if (!run) lead = b;
                 const bool alone = lead == b && !(b + 1 < B && s_lead[b + 1] == b);
                 pre = alone ? 0 : s_pre[lead];
@@ -1386,7 +1409,7 @@ static cudaError_t launch_attend_t(const KvAttendArgs &a, const ApWork &w, int s
     static std::atomic<int> done[kMaxDevices];
     auto *plan = attend_plan_kernel<C::QR, C::PAIRS, C::PG>;
     cudaError_t e = once_per_device(done, [plan] {
-        const cudaError_t x = cudaFuncSetAttribute(plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (10 * 4096 + 1) * 4);
+        const cudaError_t x = cudaFuncSetAttribute(plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (10 * AP_MAXB + 1) * 4);
         return x != cudaSuccess ? x : cudaFuncSetAttribute(attend_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     });
     if (e != cudaSuccess) return e;
