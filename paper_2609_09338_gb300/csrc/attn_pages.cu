@@ -565,16 +565,20 @@ __device__ __forceinline__ void ap_st16(uint32_t addr, const uint32_t (&r)[16]) 
                  : "memory");
 }
 
-// Waits for a phase, about a second at most: then, or when another wait of the block has
-// run out, false.  (What is not needed for a phase that has ended is a call: the loops'
-// code has to stay in the instruction cache.)
-__device__ __noinline__ bool ap_wait_long(uint64_t *bar, uint32_t parity, int *abort, int32_t *status) {
+// Waits for a phase, about a second at most, or a second without a change of `steps`, where that is given: then, or when
+// another wait of the block has run out, false.
+__device__ __forceinline__ bool ap_wait_limit(uint64_t *bar, uint32_t parity, const int *steps, int *abort, int32_t *status) {
     long long t0 = 0;
+    int seen = 0;
     for (int i = 0; !mbar_try_wait(bar, parity);) {
         if (++i < 64) continue;
         if (*(volatile int *)abort) return false;
         const long long t = clock64();
-        if (!t0) t0 = t;
+        const int now = steps ? *(const volatile int *)steps : 0;
+        if (!t0 || now != seen) {
+            t0 = t;
+            seen = now;
+        }
         if (t - t0 > 2000000000LL) {
             *(volatile int *)abort = 1;
             set_status(status, OSPREY_ERR_TIMEOUT);
@@ -583,6 +587,14 @@ __device__ __noinline__ bool ap_wait_long(uint64_t *bar, uint32_t parity, int *a
         i = 0;
     }
     return true;
+}
+// What is not needed for a phase that has ended is a call: the loops' code has to stay in the instruction cache.
+__device__ __noinline__ bool ap_wait_long(uint64_t *bar, uint32_t parity, int *abort, int32_t *status) {
+    return ap_wait_limit(bar, parity, nullptr, abort, status);
+}
+// A wait as long as another warp's work, which may be seconds: `steps` are the tiles that it is through with.
+__device__ __noinline__ bool ap_wait_work(uint64_t *bar, uint32_t parity, const int *steps, int *abort, int32_t *status) {
+    return ap_wait_limit(bar, parity, steps, abort, status);
 }
 __device__ __forceinline__ bool ap_wait(uint64_t *bar, uint32_t parity, int *abort, int32_t *status) {
     return mbar_try_wait(bar, parity & 1) || ap_wait_long(bar, parity & 1, abort, status);
@@ -617,7 +629,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     uint8_t *sq = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023), *ring = sq + C::QB;
     __shared__ __align__(8) uint64_t full2[NS], freed2[NS], full1[2 * NSS], freed1[2 * NSS], sfull[2], pready[4], qready[2], odone[2], handed;
     // units with a value that is not finite among keys that not every row sees (a stream is a few units ahead at most)
-    __shared__ int s_abort, s_odd[3][16];
+    __shared__ int s_abort, s_steps, s_odd[3][16];
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = a.Hq / a.Hkv, lg = __ffs(G) - 1;
@@ -639,7 +651,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 mbar_init(&odone[i], 1);
             }
             mbar_init(&handed, 1);
-            s_abort = 0;
+            s_abort = s_steps = 0;
             for (int i = 0; i < 48; ++i) s_odd[0][i] = -1;
             mbar_fence_init();
         }
@@ -854,8 +866,9 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                         seg ^= 2;
                         np ^= (uint32_t)(k.k1 - k.k0 & 1) << 1;
                     }
-                    go = wait(&handed, 0);
+                    go = ap_wait_work(&handed, 0, &s_steps, &s_abort, a.status);
                 } else {
+                    int steps = 0;
                     while (go && next(k)) {
 #pragma unroll 1
                         for (int s = 0; s < 2 && go; ++s) {
@@ -875,6 +888,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                             }
                             if (t + 1 < k.k1) ks.step(r.n);
                             vs.step(r.n);
+                            *(volatile int *)&s_steps = ++steps;
                         }
                     }
                     mbar_arrive(&handed);
