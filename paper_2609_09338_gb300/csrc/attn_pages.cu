@@ -67,10 +67,11 @@ struct AP {
     static constexpr int QS = QP * QTB, QB = 2 * QS;           // of a stream's planes, of both
     static constexpr int NS = (224 * 1024 - QB) / TB > 16 ? 16 : (224 * 1024 - QB) / TB, NSS = NS / 2;   // slots of K and V tiles, in turn; of one stream's
     static constexpr int SC = 128;                             // columns of a stream's scores and weights
-    // An accumulator in TMEM is cut off, not rounded, at each product's addition: 2e-8 of it a step, all of one sign.
-    // float32 queries' scores are two of them, half of the dims each, with the small planes first, and their outputs are
-    // added up in float32 after every RUN tiles (8192 keys in one accumulator: 3e-5 off).
-    static constexpr int RUN = 2;
+    // An accumulator in TMEM is cut off, not rounded, at each product's addition, 16 keys or dims: up to 2^-23 of it, all of
+    // one sign (outputs of 2^21 keys of bf16 queries in one accumulator: 1.2 % short).  So outputs are added up in float32
+    // after every RUN tiles: 2^10 additions with bf16 queries, 2^-13 where the output's own rounding is 2^-8; with float32 ones
+    // 24, and their scores are two accumulators, half of the dims each, with the small planes first.
+    static constexpr int RUN = F32 ? 2 : 128;
     static constexpr int THREADS = 384;                        // two streams' 128, their warps of products, two of copies
     static constexpr int SMEM = 224 * 1024 + 1024;             // all of an SM's, so that no other kernel's TMEM lies beside this one's
     // (with 64 rows the first operand's other 64 are whatever lies behind: no one reads what they give)
@@ -84,10 +85,12 @@ struct __align__(16) ApUnit {
     int row0, i0, nq, kvh;     // (a list's row0 is its row, b * max_rows + j)
     int seq, lead, pre, p0;
     int base;                  // position of row row0, or AP_SEEN
-    int poff, c0;              // its first part's first row in the workspace (-1: none), the worker that begins it
+    int poff, c0;              // its first part's first row in the workspace, the worker that begins it
     int poff1, stride;         // part k > 0 begins at poff1 + k * stride
-    int id, own, pad[3];       // own: the packed rows are sequence seq's
+    int id, own;               // own: the packed rows are sequence seq's
+    int direct, pad[2];        // direct: its worker writes the output, the part's place holds sums on the way
 };
+static_assert(sizeof(ApUnit) == 80, "five loads of 16 bytes");
 
 // A worker (a block for units of two streams, a stream for the others): its tiles, and the first one's unit
 struct __align__(16) ApStart {
@@ -110,7 +113,7 @@ struct ApHead {
 struct ApWork {
     ApHead *head;
     ApUnit *units;
-    int4 *parts;               // of a unit: poff, poff1, stride, how many
+    int4 *parts;               // of a unit: poff (-1: its output is written), poff1, stride, how many
     ApSeq *seqs;
     int2 *rows;                // packed rows: b * max_rows + j, position
     ApStart *start;            // [sms] workers of two streams, [2 * sms] of one
@@ -409,8 +412,8 @@ __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs
             u.poff1 = from + 2 * u.c0 * most;
             u.stride = 2 * most;
         }
-        if (segs == 1 && !other) u.poff = -1;
-        w.parts[u.id] = make_int4(u.poff, u.poff1, u.stride, segs);
+        u.direct = segs == 1 && !other;
+        w.parts[u.id] = make_int4(u.direct ? -1 : u.poff, u.poff1, u.stride, segs);
         w.units[u.id] = u;
         if (segs > 1 && !split) w.split[rank * 3 * sms + atomicAdd(&s_split, 1)] = u.id;
         for (int c = by(u.cum + d - 1, pair); c <= last; ++c) {
@@ -882,7 +885,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                         for (int t = k.k0; t < k.k1 && go; ++t) {
 #pragma unroll 1
                             for (int s = 0; s < 2 && go; ++s) {
-                                outputs(r, s, vs, min(PG, k.u.np - t * PG), t == k.k0, s == 1);
+                                outputs(r, s, vs, min(PG, k.u.np - t * PG), (t - k.k0) % C::RUN == 0, s == 1);
                                 if (t + 1 < k.k1) scores(r, s, ks, s == 1);
                                 else if (go) tc_commit(&odone[s]);
                             }
@@ -905,7 +908,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 ks.step(r.n);
 #pragma unroll 1
                 for (int t = k.k0; t < k.k1 && go; ++t) {
-                    outputs(r, me, vs, min(PG, k.u.np - t * PG), C::F32 ? (t - k.k0) % C::RUN == 0 : t == k.k0, true);
+                    outputs(r, me, vs, min(PG, k.u.np - t * PG), (t - k.k0) % C::RUN == 0, true);
                     vs.step(r.n);
                     if (t + 1 < k.k1) {
                         scores(r, me, ks, true);
@@ -1026,17 +1029,17 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 const int pos_max = u.base == AP_SEEN || a.pages ? u.base : u.base + ((u.i0 + u.nq - 1) >> lg);
                 const int32_t *list = a.pages ? a.pages + ((size_t)u.row0 * a.Hkv + u.kvh) * a.n_select : nullptr;
                 float m = -INFINITY, l = 0.f;
-                // The accumulator's outputs, to the unit's part or the call's output (all of them: `last`), added to those of the
-                // runs before.
+                // The accumulator's outputs, added to those of the runs before: to the unit's part, or (all of them: `last`) to the
+                // call's output.
                 bool added = false;
                 float m_then = 0.f;
                 auto flush = [&](bool last) {
                     const int seg_key = max((u.p0 + k.k0 * PG) * 16, pos_min + 1), seg_end = min((u.p0 + min(k.k1 * PG, u.np)) * 16, pos + 1);
                     const bool odd = last && *(volatile int *)&s_odd[two ? 2 : s][u.id & 15] == u.id && !list && u.base != AP_SEEN;
-                    const bool direct = u.poff < 0;
+                    const bool direct = u.direct;
                     const int me = two ? blockIdx.x : 2 * blockIdx.x + s, iq = q0 + r;
                     const int part = me - u.c0;
-                    const size_t prow = direct ? 0 : (size_t)(part == 0 ? u.poff : u.poff1 + part * u.stride) + (iq - u.i0);
+                    const size_t prow = (size_t)(part == 0 ? u.poff : u.poff1 + part * u.stride) + (iq - u.i0);
                     const size_t orow = ((size_t)(a.pages ? u.row0 : u.seq * a.max_rows + (iq >> lg)) * a.Hq + u.kvh * G + (iq & (G - 1))) * HD;
                     // an empty list's output is 0; other rows' without a weight, whose scores are all -inf, NaN
                     const float by = !direct || !last ? 1.f : l == 0.f ? (list && list[0] < 0 ? 0.f : NAN) : 1.f / l;
@@ -1064,25 +1067,24 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                                     if ((vr[i] & 0x7f80u) == 0x7f80u) o[i] += bf_to_f(vr[i]);
                             }
                         if (live) {
-                            if (!direct || C::F32) {
-                                float *dst = !direct ? w.o + prow * HD + c * 32 : (float *)a.out + orow + c * 32;
-                                if (C::F32 && added) {
+                            float *acc = w.o + prow * HD + c * 32;
+                            if (added) {
 #pragma unroll
-                                    for (int i = 0; i < 32; i += 4) {
-                                        const float4 x = *(const float4 *)(dst + i);
-                                        o[i] = fmaf(x.x, then, o[i]);
-                                        o[i + 1] = fmaf(x.y, then, o[i + 1]);
-                                        o[i + 2] = fmaf(x.z, then, o[i + 2]);
-                                        o[i + 3] = fmaf(x.w, then, o[i + 3]);
-                                    }
+                                for (int i = 0; i < 32; i += 4) {
+                                    const float4 x = *(const float4 *)(acc + i);
+                                    o[i] = fmaf(x.x, then, o[i]);
+                                    o[i + 1] = fmaf(x.y, then, o[i + 1]);
+                                    o[i + 2] = fmaf(x.z, then, o[i + 2]);
+                                    o[i + 3] = fmaf(x.w, then, o[i + 3]);
                                 }
+                            }
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] *= by;
+                            for (int i = 0; i < 32; ++i) o[i] *= by;
+                            if (!direct || !last || C::F32) {
+                                float *dst = direct && last ? (float *)a.out + orow + c * 32 : acc;
 #pragma unroll
                                 for (int i = 0; i < 32; i += 4) *(float4 *)(dst + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                             } else {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] *= by;
                                 uint16_t *dst = (uint16_t *)a.out + orow + c * 32;
 #pragma unroll
                                 for (int i = 0; i < 32; i += 8)
@@ -1120,9 +1122,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     wait(&sfull[s], ns++);
                     __syncwarp();
                     tc_fence_after();
-                    if constexpr (C::F32) {   // the scores came behind the products of the tile before
-                        if (t > k.k0 && (t - k.k0) % C::RUN == 0 && warp_live) flush(false);
-                    }
+                    // (the scores came behind the products of the tile before)
+                    if (t > k.k0 && (t - k.k0) % C::RUN == 0 && warp_live) flush(false);
                     // V of keys that not every query sees: what none sees counts as 0, whatever the page holds, and what
                     // is not finite is added at the end to the queries that see it.  (Behind the wait for the scores: the
                     // tile before's V has landed then, and the barrier is in this one's phase or past it.)
