@@ -630,7 +630,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
     constexpr int W_MMA = 8, W_COPY = 10;
     extern __shared__ uint8_t raw[];
     uint8_t *sq = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023), *ring = sq + C::QB;
-    __shared__ __align__(8) uint64_t full2[NS], freed2[NS], full1[2 * NSS], freed1[2 * NSS], sfull[2], pready[4], qready[2], odone[2], handed;
+    __shared__ __align__(8) uint64_t full2[NS], freed2[NS], full1[2 * NSS], freed1[2 * NSS], sfull[2], pready[4], qready[2], odone[2], handed, drained[2];
     // units with a value that is not finite among keys that not every row sees (a stream is a few units ahead at most)
     __shared__ int s_abort, s_steps, s_odd[3][16];
     __shared__ uint32_t s_tmem;
@@ -652,6 +652,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                 mbar_init(&pready[2 + i], 4);
                 mbar_init(&qready[i], 4);
                 mbar_init(&odone[i], 1);
+                mbar_init(&drained[i], 1);
             }
             mbar_init(&handed, 1);
             s_abort = s_steps = 0;
@@ -926,8 +927,9 @@ __global__ void __launch_bounds__(C::THREADS, 1)
         const uint32_t ts = tmem + lanes + s * C::SC, to = tmem + lanes + 256 + s * 128;
         constexpr float sc = (float)((HD == 128 ? 0.08838834764831845 : 0.125) * 1.4426950408889634);
         uint32_t ns = 0, seg = 0;
+        bool go = true;   // a warp's threads leave together, a run of tiles after a wait that gave up at most
 #pragma unroll 1
-        for (int phase = C::PAIRS ? 0 : 1; phase < 2; ++phase) {
+        for (int phase = C::PAIRS ? 0 : 1; phase < 2 && go; ++phase) {
             const bool two = phase == 0;
             const ApRing rg = ring_of(two, s);
             Walk k = begin(two, s);
@@ -1098,191 +1100,203 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                     m_then = m;
                 };
 #pragma unroll 1
-                for (int t = k.k0; t < k.k1; ++t, vs.step(rg.n)) {
-                    const int key0 = (u.p0 + t * PG) * 16;
-                    const int pages = min(PG, u.np - t * PG);
-                    // keys of the tile that the thread's query, every query and any query sees
-                    int lim, lim_min, lim_max;
-                    if (list) {
-                        int n = 0, e_last = -1;
-#pragma unroll
-                        for (int p = 0; p < PG; ++p) {
-                            const int e = p < pages ? list[t * PG + p] : -1;
-                            if (e >= 0) {
-                                n = p + 1;
-                                e_last = e;
-                            }
-                        }
-                        lim = lim_min = lim_max = e_last == pos / 16 ? (n - 1) * 16 + pos % 16 + 1 : n * 16;
-                    } else {
-                        lim = min(pages * 16, pos - key0 + 1);
-                        lim_min = min(pages * 16, pos_min - key0 + 1);
-                        lim_max = min(pages * 16, pos_max - key0 + 1);
-                    }
-                    wait(&sfull[s], ns++);
-                    __syncwarp();
-                    tc_fence_after();
-                    // (the scores came behind the products of the tile before)
-                    if (t > k.k0 && (t - k.k0) % C::RUN == 0 && warp_live) flush(false);
-                    // V of keys that not every query sees: what none sees counts as 0, whatever the page holds, and what
-                    // is not finite is added at the end to the queries that see it.  (Behind the wait for the scores: the
-                    // tile before's V has landed then, and the barrier is in this one's phase or past it.)
-                    if (max(lim_min, 0) < pages * 16) {
-                        wait(&rg.full[vs.slot], vs.use);
-                        if (r >= lim_min && r < pages * 16) {
-                            uint8_t *v = ring + (rg.base + vs.slot) * TB + (r >> 4) * 2048 * NH + (r & 15) * 128;
+                for (int t0 = k.k0; t0 < k.k1 && go; t0 += C::RUN) {
+                    const int t1 = min(t0 + C::RUN, k.k1);
 #pragma unroll 1
-                            for (int c = 0; c < 8 * NH; ++c) {
-                                uint4 *x = (uint4 *)(v + (c >> 3) * 2048 + (c & 7) * 16);
-                                if (r >= lim_max) {
-                                    *x = make_uint4(0, 0, 0, 0);
-                                } else {
-                                    uint4 y = *x;
-                                    uint32_t z[4] = {y.x, y.y, y.z, y.w};
-                                    bool odd = false;
+                    for (int t = t0; t < t1; ++t, vs.step(rg.n)) {
+                        const int key0 = (u.p0 + t * PG) * 16;
+                        const int pages = min(PG, u.np - t * PG);
+                        // keys of the tile that the thread's query, every query and any query sees
+                        int lim, lim_min, lim_max;
+                        if (list) {
+                            int n = 0, e_last = -1;
 #pragma unroll
-                                    for (int q = 0; q < 4; ++q) {
-                                        if ((z[q] & 0x7f80u) == 0x7f80u) z[q] &= 0xffff0000u, odd = true;
-                                        if ((z[q] & 0x7f800000u) == 0x7f800000u) z[q] &= 0xffffu, odd = true;
-                                    }
-                                    if (odd) {   // the flag first: the other stream may find zeros
-                                        *(volatile int *)&s_odd[two ? 2 : s][u.id & 15] = u.id;
-                                        __threadfence_block();
-                                        *x = make_uint4(z[0], z[1], z[2], z[3]);
-                                    }
+                            for (int p = 0; p < PG; ++p) {
+                                const int e = p < pages ? list[t * PG + p] : -1;
+                                if (e >= 0) {
+                                    n = p + 1;
+                                    e_last = e;
                                 }
                             }
-                            ap_fence_smem();
+                            lim = lim_min = lim_max = e_last == pos / 16 ? (n - 1) * 16 + pos % 16 + 1 : n * 16;
+                        } else {
+                            lim = min(pages * 16, pos - key0 + 1);
+                            lim_min = min(pages * 16, pos_min - key0 + 1);
+                            lim_max = min(pages * 16, pos_max - key0 + 1);
                         }
+                        wait(&sfull[s], ns++);
                         __syncwarp();
-                    }
-                    if (warp_live) {
-                        if (lim_min < KEYS) {   // of the whole tile: a warp's threads take the same way.  What is not seen is -inf.
+                        tc_fence_after();
+                        // V of keys that not every query sees: what none sees counts as 0, whatever the page holds, and what
+                        // is not finite is added at the end to the queries that see it.  (Behind the wait for the scores: the
+                        // tile before's V has landed then, and the barrier is in this one's phase or past it.)
+                        if (max(lim_min, 0) < pages * 16) {
+                            wait(&rg.full[vs.slot], vs.use);
+                            if (r >= lim_min && r < pages * 16) {
+                                uint8_t *v = ring + (rg.base + vs.slot) * TB + (r >> 4) * 2048 * NH + (r & 15) * 128;
 #pragma unroll 1
-                            for (int c = max(lim_min, 0) & ~15; c < KEYS; c += 16) {
-                                float x[16];
-                                tc_ld16(ts + c, x);
-                                tc_ld_wait();
-                                tc_ld_tie(x);
+                                for (int c = 0; c < 8 * NH; ++c) {
+                                    uint4 *x = (uint4 *)(v + (c >> 3) * 2048 + (c & 7) * 16);
+                                    if (r >= lim_max) {
+                                        *x = make_uint4(0, 0, 0, 0);
+                                    } else {
+                                        uint4 y = *x;
+                                        uint32_t z[4] = {y.x, y.y, y.z, y.w};
+                                        bool odd = false;
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) x[i] = c + i < lim ? x[i] : -INFINITY;
-                                tc_st16(ts + c, x);
-                                if constexpr (C::F32) {
-                                    tc_ld16(ts + 64 + c, x);
+                                        for (int q = 0; q < 4; ++q) {
+                                            if ((z[q] & 0x7f80u) == 0x7f80u) z[q] &= 0xffff0000u, odd = true;
+                                            if ((z[q] & 0x7f800000u) == 0x7f800000u) z[q] &= 0xffffu, odd = true;
+                                        }
+                                        if (odd) {   // the flag first: the other stream may find zeros
+                                            *(volatile int *)&s_odd[two ? 2 : s][u.id & 15] = u.id;
+                                            __threadfence_block();
+                                            *x = make_uint4(z[0], z[1], z[2], z[3]);
+                                        }
+                                    }
+                                }
+                                ap_fence_smem();
+                            }
+                            __syncwarp();
+                        }
+                        if (warp_live) {
+                            if (lim_min < KEYS) {   // of the whole tile: a warp's threads take the same way.  What is not seen is -inf.
+#pragma unroll 1
+                                for (int c = max(lim_min, 0) & ~15; c < KEYS; c += 16) {
+                                    float x[16];
+                                    tc_ld16(ts + c, x);
                                     tc_ld_wait();
                                     tc_ld_tie(x);
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) x[i] = c + i < lim ? x[i] : 0.f;
-                                    tc_st16(ts + 64 + c, x);
+                                    for (int i = 0; i < 16; ++i) x[i] = c + i < lim ? x[i] : -INFINITY;
+                                    tc_st16(ts + c, x);
+                                    if constexpr (C::F32) {
+                                        tc_ld16(ts + 64 + c, x);
+                                        tc_ld_wait();
+                                        tc_ld_tie(x);
+#pragma unroll
+                                        for (int i = 0; i < 16; ++i) x[i] = c + i < lim ? x[i] : 0.f;
+                                        tc_st16(ts + 64 + c, x);
+                                    }
                                 }
-                            }
-                            tc_st_wait();
-                        }
-                        // 32 scores at a time, twice: for the largest, and for the weights.  (The block's loops have to stay in the
-                        // instruction cache: all 128 scores in registers, once, made prompts 468 us instead of 418, 64 at a time
-                        // 430, the weights' loop unrolled 424, the first loop rolled 463.)
-                        uint32_t v[32];
-                        auto scores = [&](int c) {
-                            ap_ld32(ts + c * 32, v);
-                            tc_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(v[i]));   // not before the wait
-                            if constexpr (C::F32) {
-                                uint32_t x[32];
-                                ap_ld32(ts + 64 + c * 32, x);
-                                tc_ld_wait();
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    asm volatile("" : "+r"(x[i]));
-                                    v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(x[i]));
-                                }
-                            }
-                        };
-                        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int c = 0; c < KEYS / 32; ++c) {
-                            scores(c);
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2)
-                                asm("max.f32 %0, %0, %1, %2;" : "+f"(t4[i / 2 & 3]) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
-                        }
-                        const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * sc;
-                        const float was = m;
-                        if (m == -INFINITY || top > m + AP_OVER) m = top;
-                        const bool moved = m != was && was != -INFINITY;
-                        if (__any_sync(0xffffffffu, moved)) {   // every product of this stream has ended: the scores came behind them
-                            const float f = moved ? ap_ex2(was - m) : 1.f;
-                            l *= f;
-#pragma unroll 1
-                            for (int c = 0; c < HD / 16; ++c) {
-                                float x[16];
-                                tc_ld16(to + c * 16, x);
-                                tc_ld_wait();
-                                tc_ld_tie(x);
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) x[i] *= f;
-                                tc_st16(to + c * 16, x);
-                            }
-                        }
-                        const float ref = m == -INFINITY ? 0.f : m;
-                        f2 sum[2] = {0ull, 0ull};
-                        const f2 sc2 = mk2(sc, sc), rf2 = mk2(-ref, -ref);
-#pragma unroll 1
-                        for (int c = 0; c < KEYS / 32; ++c) {
-                            scores(c);
-                            uint32_t p[PP][16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                float e0, e1;
-                                un2(fma2(mk2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc2, rf2), e0, e1);
-                                e0 = ap_ex2(e0);
-                                e1 = ap_ex2(e1);
-                                p[0][i] = kv8_bf2(e0, e1);
-                                if constexpr (PP == 3) {
-                                    const float d0 = e0 - bf_lo(p[0][i]), d1 = e1 - bf_hi(p[0][i]);
-                                    p[1][i] = kv8_bf2(d0, d1);
-                                    p[2][i] = kv8_bf2(d0 - bf_lo(p[1][i]), d1 - bf_hi(p[1][i]));
-                                }
-                                sum[i & 1] = add2(sum[i & 1], mk2(e0, e1));
-                            }
-                            ap_st16(ts + c * 32, p[0]);
-                            if constexpr (PP == 3) {
-                                ap_st16(ts + c * 32 + 16, p[1]);
-                                ap_st16(ts + KEYS + c * 16, p[2]);
-                            }
-                            if (c & 1) {   // 64 keys' weights: their products may begin
                                 tc_st_wait();
-                                tc_fence_before();
-                                __syncwarp();
-                                if (lane == 0) mbar_arrive(&pready[2 * (c >> 1) + s]);
                             }
-                        }
-                        float x0, x1, y0, y1;
-                        un2(sum[0], x0, x1);
-                        un2(sum[1], y0, y1);
-                        l += (x0 + x1) + (y0 + y1);
-                    }
-                    if (!warp_live) {
-                        __syncwarp();
-                        if (lane == 0)
+                            // 32 scores at a time, twice: for the largest, and for the weights.  (The block's loops have to stay in the
+                            // instruction cache: all 128 scores in registers, once, made prompts 468 us instead of 418, 64 at a time
+                            // 430, the weights' loop unrolled 424, the first loop rolled 463.)
+                            uint32_t v[32];
+                            auto scores = [&](int c) {
+                                ap_ld32(ts + c * 32, v);
+                                tc_ld_wait();
 #pragma unroll
-                            for (int h = 0; h < C::PARTS; ++h) mbar_arrive(&pready[2 * h + s]);
+                                for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(v[i]));   // not before the wait
+                                if constexpr (C::F32) {
+                                    uint32_t x[32];
+                                    ap_ld32(ts + 64 + c * 32, x);
+                                    tc_ld_wait();
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) {
+                                        asm volatile("" : "+r"(x[i]));
+                                        v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(x[i]));
+                                    }
+                                }
+                            };
+                            float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                            for (int c = 0; c < KEYS / 32; ++c) {
+                                scores(c);
+#pragma unroll
+                                for (int i = 0; i < 32; i += 2)
+                                    asm("max.f32 %0, %0, %1, %2;" : "+f"(t4[i / 2 & 3]) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
+                            }
+                            const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * sc;
+                            const float was = m;
+                            if (m == -INFINITY || top > m + AP_OVER) m = top;
+                            const bool moved = m != was && was != -INFINITY;
+                            if (__any_sync(0xffffffffu, moved)) {   // every product of this stream has ended: the scores came behind them
+                                const float f = moved ? ap_ex2(was - m) : 1.f;
+                                l *= f;
+#pragma unroll 1
+                                for (int c = 0; c < HD / 16; ++c) {
+                                    float x[16];
+                                    tc_ld16(to + c * 16, x);
+                                    tc_ld_wait();
+                                    tc_ld_tie(x);
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) x[i] *= f;
+                                    tc_st16(to + c * 16, x);
+                                }
+                            }
+                            const float ref = m == -INFINITY ? 0.f : m;
+                            f2 sum[2] = {0ull, 0ull};
+                            const f2 sc2 = mk2(sc, sc), rf2 = mk2(-ref, -ref);
+#pragma unroll 1
+                            for (int c = 0; c < KEYS / 32; ++c) {
+                                scores(c);
+                                uint32_t p[PP][16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    float e0, e1;
+                                    un2(fma2(mk2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc2, rf2), e0, e1);
+                                    e0 = ap_ex2(e0);
+                                    e1 = ap_ex2(e1);
+                                    p[0][i] = kv8_bf2(e0, e1);
+                                    if constexpr (PP == 3) {
+                                        const float d0 = e0 - bf_lo(p[0][i]), d1 = e1 - bf_hi(p[0][i]);
+                                        p[1][i] = kv8_bf2(d0, d1);
+                                        p[2][i] = kv8_bf2(d0 - bf_lo(p[1][i]), d1 - bf_hi(p[1][i]));
+                                    }
+                                    sum[i & 1] = add2(sum[i & 1], mk2(e0, e1));
+                                }
+                                ap_st16(ts + c * 32, p[0]);
+                                if constexpr (PP == 3) {
+                                    ap_st16(ts + c * 32 + 16, p[1]);
+                                    ap_st16(ts + KEYS + c * 16, p[2]);
+                                }
+                                if (c & 1) {   // 64 keys' weights: their products may begin
+                                    tc_st_wait();
+                                    tc_fence_before();
+                                    __syncwarp();
+                                    if (lane == 0) mbar_arrive(&pready[2 * (c >> 1) + s]);
+                                }
+                            }
+                            float x0, x1, y0, y1;
+                            un2(sum[0], x0, x1);
+                            un2(sum[1], y0, y1);
+                            l += (x0 + x1) + (y0 + y1);
+                        }
+                        if (!warp_live) {
+                            __syncwarp();
+                            if (lane == 0)
+#pragma unroll
+                                for (int h = 0; h < C::PARTS; ++h) mbar_arrive(&pready[2 * h + s]);
+                        }
                     }
+                    // ------------------------------------------------ the run's outputs
+                    // (the next tile's scores come behind the products of all before)
+                    if (t1 < k.k1) wait(&sfull[s], ns);
+                    else wait(&odone[s], seg++);
+                    go = __all_sync(0xffffffffu, !*(volatile int *)&s_abort);   // (a tile each: prompts took 8 % longer)
+                    tc_fence_after();
+                    if (go && warp_live) flush(t1 == k.k1);
                 }
-                // ------------------------------------------------ the unit's outputs
-                wait(&odone[s], seg++);
-                __syncwarp();
-                tc_fence_after();
-                if (warp_live) flush(true);
             }
         }
     }
     __syncwarp();
-    if (s_abort && tid == 0) {   // let what is on its way land before the block leaves; its outputs are cleared
-        *(volatile int *)&w.head->bad = 2;
-        for (int ph = 0; ph < 2; ++ph) {
-            for (int i = 0; i < NS && C::PAIRS; ++i) mbar_wait(&full2[i], ph, 20000000LL);
-            for (int i = 0; i < 2 * NSS; ++i) mbar_wait(&full1[i], ph, 20000000LL);
+    __syncthreads();
+    if (s_abort) {   // every wait has ended, one of them too early: the call's outputs are cleared, and the block stays until its
+                     // products and its copies are through
+        if ((warp == W_MMA || warp == W_MMA + 1) && tc_elect()) {
+            tc_commit(&drained[warp - W_MMA]);
+            mbar_wait(&drained[warp - W_MMA], 0, 20000000LL);
+        }
+        if (tid == 0) {
+            *(volatile int *)&w.head->bad = 2;
+            for (int ph = 0; ph < 2; ++ph) {
+                for (int i = 0; i < NS && C::PAIRS; ++i) mbar_wait(&full2[i], ph, 20000000LL);
+                for (int i = 0; i < 2 * NSS; ++i) mbar_wait(&full1[i], ph, 20000000LL);
+            }
         }
     }
     tc_fence_before();

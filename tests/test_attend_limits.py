@@ -80,3 +80,57 @@ def test_one_limit_for_all_of_the_shared_units_is_caught():
     for seed in range(5):
         m = Timed(random.Random(seed), [60, 1, 90], [[3], [2]], 10, 5, "one limit for all of the shared units")
         assert m.longest() > 3 * _most(10)
+
+
+class Ending(Model):
+    """A wait gives up, then others as they find out; the block leaves.  Thread 0 is one of the first stream's weights'."""
+
+    def leave(self, at):
+        """`at`: how many steps come before some wait gives up."""
+        actors = {i: [a, lambda: True] for i, a in enumerate(
+            [self.copies(0), self.copies(1), self.products(0), self.products(1), self.weights(0), self.weights(1)])}
+        abort = seen_by_thread_0 = False
+        while actors:
+            blocked = [i for i, (_, c) in actors.items() if not c()]
+            give_up = blocked if abort or at <= 0 else []
+            ready = [i for i in actors if i not in blocked] + ["land"] * bool(self.flying) + ["execute"] * bool(self.queue)
+            at -= 1
+            i = self.rng.choice(ready + give_up)
+            if i == "land":
+                self.land()
+            elif i == "execute":
+                self.execute()
+            else:
+                if i in blocked:
+                    abort = True
+                    del actors[i]
+                else:
+                    try:
+                        actors[i][1] = next(actors[i][0])
+                        continue
+                    except StopIteration:
+                        del actors[i]
+                if i == 4:
+                    seen_by_thread_0 = abort
+        told = seen_by_thread_0 if self.bad == "thread 0 looks when it is through" else abort
+        while told and (self.queue or self.flying):        # stays until these are through
+            self.land() if self.flying else self.execute()
+        return abort, told, len(self.queue) + len(self.flying)
+
+
+def _endings(bad=None):
+    for seed in range(300):
+        rng = random.Random(seed)
+        m = Ending(rng, [3, 1, 2], [[2], [2, 9]], 10, 5, bad)
+        yield m.leave(rng.randint(0, 400))
+
+
+def test_a_wait_that_gives_up_is_told_and_nothing_is_in_flight_when_the_block_leaves():
+    ended = list(_endings())
+    assert sum(a for a, _, _ in ended) > 100
+    for abort, told, left in ended:
+        assert told == abort and left == 0
+
+
+def test_looking_for_it_before_all_are_through_is_caught():
+    assert sum(abort and not told for abort, told, _ in _endings("thread 0 looks when it is through")) > 5
