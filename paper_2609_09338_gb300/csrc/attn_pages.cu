@@ -731,7 +731,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             }
             if (bad) {
                 *(volatile int *)((!a.pages && p < x.pre ? w.bad_pre : w.bad) + seq) = 1;
-                *(volatile int *)&w.head->bad = 1;
+                atomicMax(&w.head->bad, 1);
             }
             return id;
         };
@@ -1292,7 +1292,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             mbar_wait(&drained[warp - W_MMA], 0, 20000000LL);
         }
         if (tid == 0) {
-            *(volatile int *)&w.head->bad = 2;
+            atomicMax(&w.head->bad, 2);   // (another block's bad page may come later)
             for (int ph = 0; ph < 2; ++ph) {
                 for (int i = 0; i < NS && C::PAIRS; ++i) mbar_wait(&full2[i], ph, 20000000LL);
                 for (int i = 0; i < 2 * NSS; ++i) mbar_wait(&full1[i], ph, 20000000LL);

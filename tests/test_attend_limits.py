@@ -1,6 +1,8 @@
 """How long the waits of the attention over the bf16 cache may last (csrc/attn_pages.cu): each ends, or its limit is
 renewed, within a bounded number of products, however much work a block has."""
+import os
 import random
+import re
 
 import pytest
 
@@ -134,3 +136,13 @@ def test_a_wait_that_gives_up_is_told_and_nothing_is_in_flight_when_the_block_le
 
 def test_looking_for_it_before_all_are_through_is_caught():
     assert sum(abort and not told for abort, told, _ in _endings("thread 0 looks when it is through")) > 5
+
+
+def test_a_bad_page_does_not_take_back_that_all_is_cleared():
+    """head->bad: 1 of a bad page, 2 of a wait that gave up, from any blocks in any order: every change raises it."""
+    src = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_09338_gb300", "csrc", "attn_pages.cu")
+    with open(src) as f:
+        text = f.read()
+    kernel = text[text.index("    attend_kernel(const __grid_constant__"):text.index("void __launch_bounds__(512, 2) attend_join_kernel")]
+    assert len(re.findall(r"atomicMax\(&w\.head->bad, [12]\)", kernel)) == 2
+    assert len(re.findall(r"head->bad", kernel)) == 2
