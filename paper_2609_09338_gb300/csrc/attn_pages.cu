@@ -43,6 +43,7 @@ namespace osp {
 
 constexpr float AP_OVER = 8.f;        // a weight is at most 2^AP_OVER before its reference moves
 constexpr int AP_SEEN = 1 << 30;      // position of a row that sees every key of its unit
+constexpr int AP_NONE = -32;          // of one whose list is none, below every page: whoever reads the list refuses its entries
 // What a unit costs beside its tiles, in tiles: its queries' loads, its outputs' stores and the waits
 // between (with tiles alone dealt out evenly, 1..8 rows of 96 sequences: blocks ended between 57 and 92 us, 129 us a call
 // instead of 116).  Units of lists are much alike, and whole numbers of tiles more even without it (132 us instead of 140).
@@ -84,7 +85,7 @@ struct __align__(16) ApUnit {
     int cum, np;               // tiles of the units before, of its class, and what they cost beside; pages
     int row0, i0, nq, kvh;     // (a list's row0 is its row, b * max_rows + j)
     int seq, lead, pre, p0;
-    int base;                  // position of row row0, or AP_SEEN
+    int base;                  // position of row row0, or AP_SEEN, AP_NONE
     int poff, c0;              // its first part's first row in the workspace, the worker that begins it
     int poff1, stride;         // part k > 0 begins at poff1 + k * stride
     int id, own;               // own: the packed rows are sequence seq's
@@ -221,9 +222,67 @@ __device__ __forceinline__ int ap_tiles(int base, int queries, int lg, const ApC
     return ap_ceil((base + (i >> lg)) / 16 + 1 - p0, PG);
 }
 
+// Which of a warp's lanes (of those in `todo`) have a list with an entry past the row's pages, from np on, that is not -1:
+// four lists at a time, 256 entries each.  64 rows of 8 heads with 127 entries behind one page: 3 us; 512 rows 17 (a list
+// a lane: 8 and 70); one row with 65535: 275.  (In the attention's copying warps, inlined or called, it moved the other
+// warps' loops so that prompts took 444 us instead of 419.)
+__device__ __noinline__ uint32_t ap_behind(const int32_t *pages, int list, int np, uint32_t todo, int n) {
+    const int lane = threadIdx.x & 31;
+    const bool wide = n % 4 == 0 && (uintptr_t)pages % 16 == 0;
+    uint32_t found = 0;
+    while (todo) {
+        const int32_t *x[4];
+        int from[4], low = n;
+        uint32_t bits[4], odd[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            bits[u] = todo & (0u - todo);   // 0: no more
+            const int src = bits[u] ? __ffs(todo) - 1 : 0;
+            todo ^= bits[u];
+            x[u] = pages + (size_t)__shfl_sync(0xffffffffu, list, src) * n;
+            from[u] = __shfl_sync(0xffffffffu, np, src);
+            if (!bits[u]) from[u] = n;
+            low = min(low, from[u]);
+        }
+        if (wide) {
+            for (int i = (low & ~3) + lane * 4; i < n; i += 256) {
+                int4 v[4][2];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int at = i + 128 * k;
+                        v[u][k] = at < n && at + 3 >= from[u] ? *(const int4 *)(x[u] + at) : make_int4(-1, -1, -1, -1);
+                    }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int at = i + 128 * k - from[u];   // of the first one, behind the list's pages
+                        odd[u] |= (at >= 0 ? ~v[u][k].x : 0) | (at >= -1 ? ~v[u][k].y : 0) | (at >= -2 ? ~v[u][k].z : 0) | ~v[u][k].w;
+                    }
+            }
+        } else {
+            for (int i = low + lane; i < n; i += 64) {
+                int v[4][2];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) v[u][k] = i + 32 * k < n && i + 32 * k >= from[u] ? x[u][i + 32 * k] : -1;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) odd[u] |= ~v[u][0] | ~v[u][1];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (__any_sync(0xffffffffu, odd[u] != 0)) found |= bits[u];
+    }
+    return found;
+}
+
 // One block lists the units.  Those of two streams and those of one are two classes, each
 // with tiles, units and workers of its own; in a class the prefixes' come first.
-template <int QR, bool PAIRS, int PG>
+template <int QR, bool PAIRS, int PG, bool LISTS>
 __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs a, const ApWork w, int sms) {
     extern __shared__ unsigned long long s_dyn[];
     const int B = a.B, Hkv = a.Hkv, lg = __ffs(a.Hq / Hkv) - 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -239,7 +298,8 @@ __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs
     for (int b = tid; b < B; b += AP_PLAN) s_cnt[b] = 0;
     pdl_wait();
     pdl_trigger();
-    const bool lists = a.pages != nullptr, split = a.share && (a.max_rows << lg) < AP_SHARE;
+    constexpr bool lists = LISTS;
+    const bool split = !LISTS && a.share && (a.max_rows << lg) < AP_SHARE;
     for (int b0 = 0; b0 < B; b0 += AP_PLAN) {
         const int b = b0 + tid;
         bool begins = false;   // a run, or none of them: its first sequence is not the one before's
@@ -493,7 +553,8 @@ __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs
             for (int k0 = part * 32; k0 < cnt * Hkv; k0 += 32 * wide) {
                 const int k = k0 + lane, x = min((int)(((float)k + 0.5f) * fh), cnt - 1), kvh = k - x * Hkv;
                 const int xt = __shfl_sync(0xffffffffu, nt, x), xe = __shfl_sync(0xffffffffu, e, x), y = i0 + x;
-                if (k >= cnt * Hkv) continue;
+                const bool mine = k < cnt * Hkv;
+                if (!LISTS && !mine) continue;
                 u.kvh = kvh;
                 if (lists) {
                     u.id = unit + y * Hkv + kvh;
@@ -502,6 +563,8 @@ __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs
                     u.nq = 1 << lg;
                     u.base = base + y;
                     u.np = min(a.n_select, u.base / 16 + 1);
+                    const uint32_t some = __ballot_sync(0xffffffffu, mine && u.np < a.n_select);
+                    if (some && ap_behind(a.pages, u.row0 * Hkv + kvh, u.np, some, a.n_select) >> lane & 1) u.base = AP_NONE;
                 } else {
                     u.id = unit + kvh * c.units + y;
                     u.cum = cum0 + kvh * one + xe;
@@ -511,7 +574,7 @@ __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs
                     u.base = base;
                     u.np = (base + ((u.i0 + u.nq - 1) >> lg)) / 16 + 1 - u.p0;
                 }
-                put(u, c.pair, pre, xt - cost, ((int)rows + row) * a.Hq + kvh * (n << lg) + u.i0);
+                if (mine) put(u, c.pair, pre, xt - cost, ((int)rows + row) * a.Hq + kvh * (n << lg) + u.i0);
             }
         }
     }
@@ -1436,16 +1499,17 @@ static cudaError_t ap_launch(void (*k)(P...), int grid, int threads, size_t smem
 template <typename C>
 static cudaError_t launch_attend_t(const KvAttendArgs &a, const ApWork &w, int sms, cudaStream_t s) {
     static std::atomic<int> done[kMaxDevices];
-    auto *plan = attend_plan_kernel<C::QR, C::PAIRS, C::PG>;
-    cudaError_t e = once_per_device(done, [plan] {
-        const cudaError_t x = cudaFuncSetAttribute(plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (10 * AP_MAXB + 1) * 4);
+    auto *rows = attend_plan_kernel<C::QR, C::PAIRS, C::PG, false>, *lists = attend_plan_kernel<C::QR, C::PAIRS, C::PG, true>;
+    cudaError_t e = once_per_device(done, [rows, lists] {
+        cudaError_t x = cudaFuncSetAttribute(rows, cudaFuncAttributeMaxDynamicSharedMemorySize, (10 * AP_MAXB + 1) * 4);
+        if (x == cudaSuccess) x = cudaFuncSetAttribute(lists, cudaFuncAttributeMaxDynamicSharedMemorySize, (10 * AP_MAXB + 1) * 4);
         return x != cudaSuccess ? x : cudaFuncSetAttribute(attend_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     });
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    const int rows = a.n_pages * a.Hkv * 16;
-    if (!tc_encode_rows(&mk, a.k_pages, rows, 16, C::HD) || !tc_encode_pages(&mv, a.v_pages, rows, C::HD)) return cudaErrorInvalidValue;
-    if ((e = ap_launch(plan, (long long)a.B * a.max_rows * a.Hq > 128 ? AP_BLOCKS : 1, AP_PLAN, (size_t)(10 * a.B + 1) * 4, s, a, w, sms)) != cudaSuccess) return e;
+    const int keys = a.n_pages * a.Hkv * 16;
+    if (!tc_encode_rows(&mk, a.k_pages, keys, 16, C::HD) || !tc_encode_pages(&mv, a.v_pages, keys, C::HD)) return cudaErrorInvalidValue;
+    if ((e = ap_launch(a.pages ? lists : rows, (long long)a.B * a.max_rows * a.Hq > 128 ? AP_BLOCKS : 1, AP_PLAN, (size_t)(10 * a.B + 1) * 4, s, a, w, sms)) != cudaSuccess) return e;
     if ((e = ap_launch(attend_kernel<C>, sms, C::THREADS, C::SMEM, s, mk, mv, a, w, sms)) != cudaSuccess) return e;
     const int by_row = a.share && a.max_rows * (a.Hq / a.Hkv) < AP_SHARE;
     const int grid = by_row ? a.B * a.max_rows : 4 * sms;

@@ -144,5 +144,4 @@ def test_a_bad_page_does_not_take_back_that_all_is_cleared():
     with open(src) as f:
         text = f.read()
     kernel = text[text.index("    attend_kernel(const __grid_constant__"):text.index("void __launch_bounds__(512, 2) attend_join_kernel")]
-    assert len(re.findall(r"atomicMax\(&w\.head->bad, [12]\)", kernel)) == 2
-    assert len(re.findall(r"head->bad", kernel)) == 2
+    assert len(re.findall(r"head->bad", kernel)) == len(re.findall(r"atomicMax\(&w\.head->bad, [12]\)", kernel)) >= 2
