@@ -176,6 +176,7 @@ int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv, int layer,
  * those that seq_len[b] + n_rows[b] positions need beside them, from a list of
  * free pages, into its row of the page table.  The pages of sequence b come behind
  * those of the sequences before it.  Nothing is appended and no length changes.
+ * (Where rows are taken back, as a draft call's are: osprey_kv_reserve_held.)
  *   share [B] int32 (device) or NULL: -1 or b, or a sequence that b begins with:
  *          b's first seq_len[b] positions (whole pages) are share[b]'s, and its
  *          ids are copied.  share[b] holds as many positions and shares none.
@@ -193,6 +194,23 @@ int osprey_kv_append_rope(const osprey_ctx *ctx, const osprey_kv *kv, int layer,
 int osprey_kv_reserve(const osprey_ctx *ctx, const osprey_kv *kv, int B, const int32_t *n_rows,
                       const int32_t *share, int64_t total_rows, const int32_t *free_pages, int n_free,
                       int32_t *n_taken, int64_t *slots, int32_t *dev_status, void *stream);
+
+/* osprey_kv_reserve where rows may be taken back (a draft call needs pages for
+ * n_new + K - 1 rows and keeps n_new; a verification rejects some): pages that a
+ * sequence holds behind its length stay its own, and new rows go to them first.
+ * Without it such a page's place gets another page, and its id is in no table and
+ * in no list any more.
+ *   held [B] int32 (device) or NULL: the pages in each sequence's row, at least
+ *          ceil(seq_len[b] / 16) of them; the call adds its own.  Of a sequence that
+ *          begins with another's pages 0 or more: the shared ones count as held
+ * A page returns to the list by free_pages[--n_taken] = id, between calls: of a
+ * finished sequence its row's held ids, but those that another still shares.
+ * Device errors: as osprey_kv_reserve (a page that rows go to whose id is out of
+ * range among them), INVALID_ARG (held as above excludes, or past the page table:
+ * that sequence gets nothing).  held of a sequence that gets nothing stays. */
+int osprey_kv_reserve_held(const osprey_ctx *ctx, const osprey_kv *kv, int B, const int32_t *n_rows,
+                           const int32_t *share, int64_t total_rows, const int32_t *free_pages, int n_free,
+                           int32_t *n_taken, int32_t *held, int64_t *slots, int32_t *dev_status, void *stream);
 
 /* Causal attention of each sequence's newest rows over the bf16 cache, one layer:
  * out = softmax(q K^T / sqrt(head_dim)) V, query head h on KV head

@@ -18,6 +18,20 @@ def reserve(table, seq_len, n_rows, free, taken, share=None):
     return table, np.array(slots, np.int64), taken
 
 
+def reserve_held(table, seq_len, n_rows, free, taken, held, share=None):
+    """The page table, the slots, n_taken and held after osprey_kv_reserve_held of a call without errors."""
+    table, slots, held = table.copy(), [], list(held)
+    for b, (length, n) in enumerate(zip(seq_len, n_rows)):
+        if share is not None and share[b] not in (-1, b):
+            table[b, :length // PAGE] = table[share[b], :length // PAGE]
+            held[b] = max(held[b], length // PAGE)
+        while held[b] * PAGE < length + n:
+            table[b, held[b]] = free[taken]
+            held[b], taken = held[b] + 1, taken + 1
+        slots += [int(table[b, t // PAGE]) * PAGE + t % PAGE for t in range(length, length + n)]
+    return table, np.array(slots, np.int64), taken, held
+
+
 def exponent(peak):
     """Smallest e >= -100 with peak <= 127 * 2^e."""
     e = -100

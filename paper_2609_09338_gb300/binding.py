@@ -91,6 +91,9 @@ _c_kv8_attend = _sig("osprey_kv8_attend", ctypes.c_int,
                       _i64, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp])
 _c_kv_reserve = _sig("osprey_kv_reserve", ctypes.c_int,
                      [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, _vp, _vp, _i64, _vp, ctypes.c_int, _vp, _vp, _vp, _vp])
+_c_kv_reserve_held = _sig("osprey_kv_reserve_held", ctypes.c_int,
+                          [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, _vp, _vp, _i64, _vp, ctypes.c_int, _vp, _vp, _vp, _vp,
+                           _vp])
 _c_kv_attend_ws = _sig("osprey_kv_attend_workspace_bytes", _sz, [_vp, ctypes.c_int, ctypes.c_int])
 _c_kv_attend = _sig("osprey_kv_attend", ctypes.c_int,
                     [_vp, ctypes.POINTER(osprey_kv), ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _vp,
@@ -147,7 +150,7 @@ _c_selftest_wait = _sig("osprey_selftest_wait_timeout", ctypes.c_int, [_i64, _vp
 
 EXPORTED = ["osprey_last_error", "osprey_create", "osprey_destroy", "osprey_draft_workspace_bytes",
             "osprey_kv_append", "osprey_kv_append_rope", "osprey_kv8_append", "osprey_kv8_attend",
-            "osprey_kv_reserve", "osprey_kv_attend_workspace_bytes", "osprey_kv_attend", "osprey_kv_bound",
+            "osprey_kv_reserve", "osprey_kv_reserve_held", "osprey_kv_attend_workspace_bytes", "osprey_kv_attend", "osprey_kv_bound",
             "osprey_kv_select_workspace_bytes", "osprey_kv_select", "osprey_kv_attend_selected_workspace_bytes",
             "osprey_kv_attend_selected",
             "osprey_draft_kv8_workspace_bytes", "osprey_draft_step_kv8", "osprey_draft_step", "osprey_draft_step_hidden", "osprey_draft_step_topk",
@@ -546,9 +549,10 @@ def _kv_queries(ctx: Ctx, B, n_rows, q, workspace, status):
 
 def osprey_kv_reserve(ctx: Ctx, kv: KvCache, n_rows: torch.Tensor, free_pages: torch.Tensor, n_taken: torch.Tensor,
                       status: torch.Tensor, share: torch.Tensor | None = None, slots: torch.Tensor | None = None,
-                      total_rows: int | None = None, stream=None):
+                      total_rows: int | None = None, stream=None, held: torch.Tensor | None = None):
     """Pages for each sequence's n_rows new rows, from free_pages[n_taken:] into the page table; slots [total] int64 get
-    the rows' places.  total_rows (the sum of n_rows) is needed where slots is not given."""
+    the rows' places.  total_rows (the sum of n_rows) is needed where slots is not given.  held [B] int32: the pages in each
+    sequence's row, updated; needed where rows are taken back, whose pages are lost without it (osprey_kv_reserve_held)."""
     B = kv.page_table.shape[0]
     if total_rows is None:
         if slots is None:
@@ -562,10 +566,12 @@ def osprey_kv_reserve(ctx: Ctx, kv: KvCache, n_rows: torch.Tensor, free_pages: t
         _need(share, torch.int32, (B,), "share", False)
     if slots is not None:
         _need(slots, torch.int64, (total_rows,), "slots", False)
-    _on_device(kv, n_rows, free_pages, n_taken, status, share, slots)
+    if held is not None:
+        _need(held, torch.int32, (B,), "held", False)
+    _on_device(kv, n_rows, free_pages, n_taken, status, share, slots, held)
     kvs = _kv_struct(ctx, kv)
-    _check(_c_kv_reserve(ctx.handle, ctypes.byref(kvs), B, _ptr(n_rows), _ptr(share), total_rows, _ptr(free_pages),
-                         free_pages.numel(), _ptr(n_taken), _ptr(slots), _ptr(status), _stream(stream)))
+    _check(_c_kv_reserve_held(ctx.handle, ctypes.byref(kvs), B, _ptr(n_rows), _ptr(share), total_rows, _ptr(free_pages),
+                              free_pages.numel(), _ptr(n_taken), _ptr(held), _ptr(slots), _ptr(status), _stream(stream)))
 
 
 def osprey_kv_attend_workspace_bytes(ctx: Ctx, B: int, max_rows: int) -> int:

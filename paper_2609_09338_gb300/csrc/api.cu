@@ -462,6 +462,12 @@ static int kv_queries_check(const Dims &D, const void *q, int dtype, int64_t &q_
 extern "C" int osprey_kv_reserve(const osprey_ctx *ctx, const osprey_kv *kv, int B, const int32_t *n_rows,
                                  const int32_t *share, int64_t total_rows, const int32_t *free_pages, int n_free,
                                  int32_t *n_taken, int64_t *slots, int32_t *dev_status, void *stream) {
+    return osprey_kv_reserve_held(ctx, kv, B, n_rows, share, total_rows, free_pages, n_free, n_taken, nullptr, slots, dev_status, stream);
+}
+
+extern "C" int osprey_kv_reserve_held(const osprey_ctx *ctx, const osprey_kv *kv, int B, const int32_t *n_rows,
+                                      const int32_t *share, int64_t total_rows, const int32_t *free_pages, int n_free,
+                                      int32_t *n_taken, int32_t *held, int64_t *slots, int32_t *dev_status, void *stream) {
     g_err[0] = 0;
     if (!ctx || !kv) return fail(OSPREY_ERR_INVALID_ARG, "null context or kv");
     if (B == 0) return OSPREY_OK;
@@ -472,7 +478,7 @@ extern "C" int osprey_kv_reserve(const osprey_ctx *ctx, const osprey_kv *kv, int
     if (kv->max_pages_per_seq < 1 || kv->max_pages_per_seq >= (1 << 26) || kv->n_pages < 1)
         return fail(OSPREY_ERR_INVALID_ARG, "max_pages_per_seq in 1..2^26 - 1 and n_pages >= 1 required");
     const KvReserveArgs a{B, n_rows, kv->seq_len, share, kv->page_table, kv->max_pages_per_seq, kv->n_pages, free_pages,
-                          n_free, n_taken, slots, (int)total_rows, dev_status};
+                          n_free, n_taken, held, slots, (int)total_rows, dev_status};
     const cudaError_t e = launch_kv_reserve(a, (cudaStream_t)stream);
     return e == cudaSuccess ? OSPREY_OK : cuda_fail(e, "kv_reserve launch");
 }

@@ -42,12 +42,13 @@ static cudaError_t pages_launch(void (*k)(P...), dim3 grid, dim3 block, int clus
 // sequences 8 us, 200 k rows of 96 12 us: dependent loads, 1 us each, barriers and the code's
 // fetch.  (Slots 128 rows a warp, a row's sequence by bisection, and two barriers of the
 // cluster: 10 and 18 us.)
-constexpr int KR_MAXB = 4096, KR_T = 1024, KR_CLUSTER = 16, KR_SMEM = (4 * KR_MAXB + 1) * 4;
+constexpr int KR_MAXB = 4096, KR_T = 1024, KR_CLUSTER = 16, KR_SMEM = (5 * KR_MAXB + 1) * 4;
 
+template <bool HELD>
 __global__ void __launch_bounds__(KR_T) kv_reserve_kernel(const KvReserveArgs a) {
     extern __shared__ int s_dyn[];
-    int *s_row = s_dyn, *s_first = s_row + KR_MAXB + 1, *s_len = s_first + KR_MAXB, *s_id = s_len + KR_MAXB;
-    // first row, first new page (-1: the sequence gets none), length, the id of the page that the rows continue
+    int *s_row = s_dyn, *s_first = s_row + KR_MAXB + 1, *s_len = s_first + KR_MAXB, *s_id = s_len + KR_MAXB, *s_held = s_id + KR_MAXB;
+    // first row, first new page (-1: the sequence gets none), length, the id of the page that the rows continue, pages held
     __shared__ long long s_part[32][2];
     __shared__ int s_bad, s_any, s_used;
     cg::cluster_group cluster = cg::this_cluster();
@@ -80,17 +81,28 @@ __global__ void __launch_bounds__(KR_T) kv_reserve_kernel(const KvReserveArgs a)
             else if (a.share[from] != -1 && a.share[from] != from) code = OSPREY_ERR_INVALID_ARG;
         }
         if (!code && (long long)len + n[i] > (long long)a.max_pages * 16) code = OSPREY_ERR_CAPACITY;
-        if (!code && len % 16 && n[i]) {   // the page that the rows continue
-            const int id = a.page_table[(size_t)b * a.max_pages + len / 16];
-            if (id < 0 || id >= a.n_pages) code = OSPREY_ERR_CAPACITY;
-            s_id[b] = id;
+        int held = code ? 0 : (len + 15) / 16;
+        if (HELD && !code) {
+            const int h = a.held[b];
+            if (h < (from != -1 && from != b ? 0 : held) || h > a.max_pages) code = OSPREY_ERR_INVALID_ARG;
+            held = max(held, h);
+        }
+        if (HELD) s_held[b] = held;
+        if (!code && n[i]) {   // pages held that the rows go to: the one that they continue, and those of rows taken back
+            const int end = HELD ? min(held, (len + n[i] + 15) / 16) : held;
+            for (int p = len / 16; p < end && !code;) {
+                const int id = a.page_table[(size_t)b * a.max_pages + p];
+                if (id < 0 || id >= a.n_pages) code = OSPREY_ERR_CAPACITY;
+                if (p == len / 16) s_id[b] = id;
+                if (!HELD || ++p == end) break;
+            }
         }
         if (code) {
             need[i] = -1;
             if (!error) error = code;
             continue;
         }
-        need[i] = (len + n[i] + 15) / 16 - (len + 15) / 16;
+        need[i] = max(0, (len + n[i] + 15) / 16 - held);
         pages += need[i];
     }
     long long ir = rows, ip = pages;
@@ -168,21 +180,22 @@ __global__ void __launch_bounds__(KR_T) kv_reserve_kernel(const KvReserveArgs a)
                 for (int i = part * 32 + lane; i < n; i += 32 * wide) a.slots[at + i] = -1;
             continue;
         }
-        const int len = s_len[b], held = (len + 15) / 16, end = (len + n + 15) / 16, from = a.share ? a.share[b] : -1;
+        const int len = s_len[b], held = HELD ? s_held[b] : (len + 15) / 16, end = (len + n + 15) / 16, from = a.share ? a.share[b] : -1;
         int32_t *row = a.page_table + (size_t)b * a.max_pages;
+        if (HELD && part == 0 && lane == 0) a.held[b] = max(held, end);
         if (from >= 0 && from != b) {
             const int32_t *src = a.page_table + (size_t)from * a.max_pages;
-            for (int p0 = part * 128; p0 < held; p0 += 128 * wide) {
+            for (int p0 = part * 128; p0 < len / 16; p0 += 128 * wide) {
                 int id[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) id[i] = p0 + 32 * i + lane < held ? src[p0 + 32 * i + lane] : 0;
+                for (int i = 0; i < 4; ++i) id[i] = p0 + 32 * i + lane < len / 16 ? src[p0 + 32 * i + lane] : 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (p0 + 32 * i + lane < held) row[p0 + 32 * i + lane] = id[i];
+                    if (p0 + 32 * i + lane < len / 16) row[p0 + 32 * i + lane] = id[i];
             }
         }
         for (int p0 = len / 16 + part * 32; p0 < end; p0 += 32 * wide) {
-            const int p = p0 + lane, id = p < held ? s_id[b] : p < end ? a.free_pages[taken + first + p - held] : 0;
+            const int p = p0 + lane, id = p >= end ? 0 : p >= held ? a.free_pages[taken + first + p - held] : !HELD || p == len / 16 ? s_id[b] : row[p];
             if (p >= held && p < end) row[p] = id;
             if (!a.slots) continue;
             const int lim = min(len + n, (p0 + 32) * 16);
@@ -199,11 +212,15 @@ cudaError_t launch_kv_reserve(const KvReserveArgs &a, cudaStream_t s) {
     const int blocks = a.B <= 128 && a.total_rows <= 1024 ? 1 : KR_CLUSTER;
     static std::atomic<int> done[kMaxDevices];
     const cudaError_t e = once_per_device(done, [] {
-        const cudaError_t x = cudaFuncSetAttribute(kv_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KR_SMEM);
-        return x != cudaSuccess ? x : cudaFuncSetAttribute(kv_reserve_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        for (auto *k : {kv_reserve_kernel<false>, kv_reserve_kernel<true>}) {
+            cudaError_t x = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, KR_SMEM);
+            if (x == cudaSuccess) x = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (x != cudaSuccess) return x;
+        }
+        return cudaSuccess;
     });
     if (e != cudaSuccess) return e;
-    return pages_launch(kv_reserve_kernel, dim3(blocks), dim3(KR_T), blocks, s, KR_SMEM, a);
+    return pages_launch(a.held ? kv_reserve_kernel<true> : kv_reserve_kernel<false>, dim3(blocks), dim3(KR_T), blocks, s, KR_SMEM, a);
 }
 
 // ---------------------------------------------------------------- bounds of a page's keys

@@ -19,6 +19,7 @@ struct KvReserveArgs {
     const int32_t *free_pages;
     int n_free;
     int32_t *n_taken;
+    int32_t *held;                             // pages of each sequence's row, or null: those that seq_len needs
     int64_t *slots;                            // may be null
     int total_rows;
     int32_t *status;
