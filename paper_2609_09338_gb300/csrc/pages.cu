@@ -208,8 +208,11 @@ __global__ void __launch_bounds__(KR_T) kv_reserve_kernel(const KvReserveArgs a)
 }
 
 cudaError_t launch_kv_reserve(const KvReserveArgs &a, cudaStream_t s) {
-    // one block where that is enough work for it, else a cluster of 16, the most there is
-    const int blocks = a.B <= 128 && a.total_rows <= 1024 ? 1 : KR_CLUSTER;
+    // One block where that is enough work for it, else a cluster of 16, the most there is.  One block and 16, us back to back:
+    // 8 rows of each of 32 sequences 5.7 and 6.1, of 48 5.8 and 5.7, of 128 7.5 and 6.2; behind a shared prefix, where a
+    // table's entries are copied, 16 rows and 4 k entries 5.4 and 5.7, 16 k 6.9 and 6.2, 96 rows and 49 k 10.4 and 6.4.
+    const bool few = a.B <= 40 && a.total_rows <= 1024 && (!a.share || (int64_t)a.B * a.max_pages <= 8192);
+    const int blocks = few ? 1 : KR_CLUSTER;
     static std::atomic<int> done[kMaxDevices];
     const cudaError_t e = once_per_device(done, [] {
         for (auto *k : {kv_reserve_kernel<false>, kv_reserve_kernel<true>}) {
