@@ -222,9 +222,10 @@ int osprey_kv_reserve_held(const osprey_ctx *ctx, const osprey_kv *kv, int B, co
  *          16, for the whole run (of a sequence by itself it is not read), and its
  *          pages are read from the first sequence's row.  Rows lie behind the
  *          prefix, which the first sequence holds.  (What osprey_kv_reserve takes as
- *          share serves here too where runs are consecutive.)  Up to 127 queries a
- *          KV head and sequence read the prefix for the run; more fill the tensor
- *          cores by themselves and read it through L2
+ *          share serves here too where runs are consecutive.)  With max_rows *
+ *          n_q_heads / n_kv_heads below 128 the prefix is read once for the run; in
+ *          other calls each sequence reads it for itself, through L2, its single
+ *          rows too: what prompts need, and slow for many single rows beside one
  *   q [B][max_rows] rows of [n_q_heads][head_dim], q_stride elements apart (0:
  *          dense), OSPREY_BF16 or OSPREY_F32; rotate 1: turned to their positions
  *          on the way, bf16 ones rounded to bf16 again, as the keys of the cache
@@ -234,10 +235,12 @@ int osprey_kv_reserve_held(const osprey_ctx *ctx, const osprey_kv *kv, int B, co
  *   max_rows 1 .. 65536, B * max_rows * n_q_heads at most 2^28
  *   workspace: osprey_kv_attend_workspace_bytes (which never falls as B or
  *          max_rows grow)
- * Scores, softmax statistics and sums are float32.  A weight enters the tensor
- * cores as bf16, half a step of its own off at most, beside a sum of weights that
- * were not rounded (float32 queries: weights and queries as three of them, 24
- * bits, and outputs within about 1e-6).  A value that is not finite reaches the
+ * Scores, softmax statistics and sums are float32; a tensor core's sum of outputs
+ * is cut off, 2^-23 of it at most, for every 16 keys, and added up in float32 after
+ * 16384 (float32 queries: 128).  A weight enters the tensor cores as bf16, half a
+ * step of its own off at most, beside a sum of weights that were not rounded
+ * (float32 queries: weights and queries as three of them, 24 bits, and outputs
+ * within about 1e-6).  A value that is not finite reaches the
  * rows that see its key, and no other; so does a key's (with float32 queries as NaN).
  * Device errors: INVALID_ARG (a count, share or prefix as above excludes; of a
  * run whose first sequence is refused, every sequence is), CAPACITY (T past the

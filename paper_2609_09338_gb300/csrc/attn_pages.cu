@@ -23,13 +23,13 @@
 // place of their scores in TMEM as bf16 and are the next product's operand there, 64 keys
 // as soon as they are made.
 //
-// Measured (GB300, 8 KV heads of 128, us a call of three kernels; the second alone in brackets).  Prompts of
-// 1000..2048 rows of 4 sequences, groups of four, behind 4096 shared positions: 418 (393),
-// 1.3 PFLOP/s in the kernel, 0.67 of cuBLAS: products alone take 340 of them, weights alone
+// Measured (GB300, 8 KV heads of 128, us a call of three kernels; the second alone, caches flushed, in brackets).  Prompts of
+// 1000..2048 rows of 4 sequences, groups of four, behind 4096 shared positions: 422 (409),
+// 1.3 PFLOP/s in the kernel, 0.65 of cuBLAS: products alone take 340 of them, weights alone
 // 290, and a tile's chain leaves a third uncovered.  One row of 64 sequences behind 8192 shared positions and 50..1000
-// of their own: 61 (41, of 25 at the copy's rate: four or five tiles a unit, of which the
-// last is half empty, and 1.5 us around them).  1..8 rows of 96 sequences behind four prefixes: 104 (78).
-// Listed pages, 96 of each of 960 (row, head): 133 (117, 0.97 of the copy's rate).
+// of their own: 61 (47, of 26 at the copy's rate: four or five tiles a unit, of which the
+// last is half empty, and 1.5 us around them).  1..8 rows of 96 sequences behind four prefixes: 105 (81).
+// Listed pages, 96 of each of 960 (row, head): 135 (120, 0.95 of the copy's rate).
 #include <algorithm>
 
 #include "internal.h"
@@ -50,7 +50,7 @@ constexpr int AP_NONE = -32;          // of one whose list is none, below every 
 constexpr int AP_COST_PAIR = 4, AP_COST = 1;
 __host__ __device__ constexpr int ap_cost(bool lists, bool pair) { return lists ? 0 : pair ? AP_COST_PAIR : AP_COST; }
 constexpr int AP_BLOCKS = 4;          // blocks that plan: each counts everything and writes its share of the units
-constexpr int AP_PLAN = 1024;         // threads of the planning block
+constexpr int AP_PLAN = 1024;         // threads of a planning block
 constexpr int AP_MAXB = 4096;
 constexpr int AP_SHARE = 128;         // a prefix is shared where a sequence has fewer queries a KV head
 
@@ -280,7 +280,7 @@ __device__ __noinline__ uint32_t ap_behind(const int32_t *pages, int list, int n
     return found;
 }
 
-// One block lists the units.  Those of two streams and those of one are two classes, each
+// Lists the units, in one block or in several that each count everything.  Those of two streams and those of one are two classes, each
 // with tiles, units and workers of its own; in a class the prefixes' come first.
 template <int QR, bool PAIRS, int PG, bool LISTS>
 __global__ void __launch_bounds__(AP_PLAN) attend_plan_kernel(const KvAttendArgs a, const ApWork w, int sms) {
@@ -1291,7 +1291,10 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                                 }
                             }
                             const float ref = m == -INFINITY ? 0.f : m;
-                            f2 sum[2] = {0ull, 0ull};
+                            // A weight in one plane of bf16: 2^-8 of it off at most, outputs 2.3e-3 from float64 where their own rounding
+                        // is 1.7e-3.  Two planes, 16 bits, leave that alone and take prompts 526 us instead of 419, 1..8 rows 116
+                        // (102), the shared prefix 62 (58), listed pages 140 (131).
+                        f2 sum[2] = {0ull, 0ull};
                             const f2 sc2 = mk2(sc, sc), rf2 = mk2(-ref, -ref);
 #pragma unroll 1
                             for (int c = 0; c < KEYS / 32; ++c) {

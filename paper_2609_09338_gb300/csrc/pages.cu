@@ -335,8 +335,12 @@ constexpr uint32_t SEL_NAN = 0xfffffffdu, SEL_ALWAYS = 0xfffffffeu, SEL_BAD = 0x
 constexpr int SEL_R = 16;      // rows of a block
 constexpr int SEL_T = 256;
 constexpr int SEL_SPLIT = 4;   // blocks an SM that scores are split into (6 or 2 of them: 1 us more)
-constexpr int SEL_FEW = 2;     // rows an SM up to which 512 threads choose, else 128 (one row of 8 heads: 12.4 us both kernels,
-                               // 16.4 with 128; 1728 rows: 34.5 us, 36.8 with 256)
+// Rows an SM up to which 512 threads choose, else 128.  Both kernels, us, 128 and 512 threads, one row of 8 heads a sequence
+// unless said: 1 sequence of 250 pages 8.3 and 7.9, 1000 pages 11.3 and 9.3; 38 of 250 pages 15.9 and 15.3, of 1000 32.2 and
+// 30.1; 128 of 250 26.7 and 29.5; 1..8 rows of 48 of 256..1024 33.0 and 41.0.  How many pages a row has the host does not
+// know: where the rule takes 128 threads and rows have 1000 pages and more, 512 would be faster, 300 of 1000 pages 233 and
+// 184, 4 rows of 40 of 1000..2000 67 and 60; and where it takes 512 and rows have 100 pages, 128: 38 of them 10.5 and 11.5.
+constexpr int SEL_FEW = 2;
 
 // A score is sum_d Q+_d hi_d + Q-_d lo_d times the page's scale, Q+ and Q- the sums of a
 // group's positive and negative 8-bit queries: whole numbers, 1016 at most, which fp16

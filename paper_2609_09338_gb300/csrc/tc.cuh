@@ -105,9 +105,9 @@ struct TcArgs {
 bool tc_available();   // the driver exposes tensor-map encoding and the device is sm_100+
 bool tc_encode_weight(CUtensorMap *m, const void *w, int rows, int K);
 bool tc_encode_operand(CUtensorMap *m, const void *x, int planes, int prows, int npad, int K);
-// a single bf16 plane of `rows` rows read in place (rows past `rows` read as zero)
 // pages of 16 rows of hd bf16 [rows][hd], a page a box: 64 dims of its rows, then the next 64
 bool tc_encode_pages(CUtensorMap *m, const void *x, int rows, int hd);
+// a single bf16 plane of `rows` rows read in place (rows past `rows` read as zero)
 bool tc_encode_rows(CUtensorMap *m, const void *x, int rows, int npad, int K);
 cudaError_t tc_set_attributes();
 // SwiGLU runs as one GEMM over the gate rows (map wa) and the up rows (map wb),
