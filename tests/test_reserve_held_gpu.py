@@ -183,3 +183,30 @@ def test_drafting_on_reserved_pages():
             for x in (fixed, moving):
                 x.kv.seq_len -= dev(np.minimum(ctx % 7 + 2, 9).astype(np.int32))
     assert int(fixed.status.item()) == 0 and int(moving.status.item()) == 0
+
+
+def test_captured_and_on_a_stream_of_its_own():
+    """A captured call goes on from what the replay before it left: lengths, held pages and the counter are on the device."""
+    B, K = 6, 8
+    s = _Server(B, 300, 30)
+    n = s.pc.ints([K] * B)
+
+    def call(stream=None):
+        s.ob.osprey_kv_reserve(s.ctx, s.kv, n, s.free_t, s.taken, s.status, total_rows=B * K, held=s.held, stream=stream)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    side = torch.cuda.Stream()
+    for step in range(40):
+        s.kv.seq_len += s.pc.ints([(step + b) % (K + 1) for b in range(B)])
+        torch.cuda.synchronize()
+        if step % 2:
+            graph.replay()
+        else:
+            call(side)
+        torch.cuda.synchronize()
+        _every_page_once(s, B)
+        lens = s.kv.seq_len.tolist()
+        assert all(h >= -(-(t + K) // 16) for h, t in zip(s.held.tolist(), lens)) and int(s.status.item()) == 0
