@@ -606,6 +606,8 @@ __device__ __forceinline__ float ap_ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// the upper halves of two floats: bf16, cut off
+__device__ __forceinline__ uint32_t ap_cut2(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
 __device__ __forceinline__ void ap_ld32(uint32_t addr, uint32_t *r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
@@ -1306,11 +1308,18 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                                     un2(fma2(mk2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc2, rf2), e0, e1);
                                     e0 = ap_ex2(e0);
                                     e1 = ap_ex2(e1);
-                                    p[0][i] = kv8_bf2(e0, e1);
-                                    if constexpr (PP == 3) {
+                                    if constexpr (PP == 1) {
+                                        p[0][i] = kv8_bf2(e0, e1);
+                                    } else {
+                                        // 24 bits in three planes, cut off, so that none has another sign, and none is 0 but of a weight
+                                        // of 0: a value of infinity stays one
+                                        p[0][i] = ap_cut2(e0, e1);
                                         const float d0 = e0 - bf_lo(p[0][i]), d1 = e1 - bf_hi(p[0][i]);
-                                        p[1][i] = kv8_bf2(d0, d1);
-                                        p[2][i] = kv8_bf2(d0 - bf_lo(p[1][i]), d1 - bf_hi(p[1][i]));
+                                        p[1][i] = ap_cut2(d0, d1);
+                                        p[2][i] = ap_cut2(d0 - bf_lo(p[1][i]), d1 - bf_hi(p[1][i]));
+                                        const uint32_t least = __vminu2(p[0][i], 0x00800080u);
+                                        p[1][i] = __vmaxu2(p[1][i], least);
+                                        p[2][i] = __vmaxu2(p[2][i], least);
                                     }
                                     sum[i & 1] = add2(sum[i & 1], mk2(e0, e1));
                                 }
