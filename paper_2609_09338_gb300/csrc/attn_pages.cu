@@ -42,6 +42,10 @@
 namespace osp {
 
 constexpr float AP_OVER = 8.f;        // a weight is at most 2^AP_OVER before its reference moves
+// From here on scores count in quarters, exactly, not in sc: the reference's rounding, half a step of it, must stay below
+// what an exponent can be (with sc alone equal scores of 1e12 gave NaN).  A step of such a score is 65 and more in the exponent,
+// so all but the largest weigh nothing either way.
+constexpr float AP_HUGE = 0x1p32f;
 constexpr int AP_SEEN = 1 << 30;      // position of a row that sees every key of its unit
 constexpr int AP_NONE = -32;          // of one whose list is none, below every page: whoever reads the list refuses its entries
 // What a unit costs beside its tiles, in tiles: its queries' loads, its outputs' stores and the waits
@@ -1274,7 +1278,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                                 for (int i = 0; i < 32; i += 2)
                                     asm("max.f32 %0, %0, %1, %2;" : "+f"(t4[i / 2 & 3]) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
                             }
-                            const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * sc;
+                            const float best = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+                            const float top = best * (fabsf(best) >= AP_HUGE ? 0.25f : sc);
                             const float was = m;
                             if (m == -INFINITY || top > m + AP_OVER) m = top;
                             const bool moved = m != was && was != -INFINITY;
@@ -1297,7 +1302,8 @@ __global__ void __launch_bounds__(C::THREADS, 1)
                         // is 1.7e-3.  Two planes, 16 bits, leave that alone and take prompts 526 us instead of 419, 1..8 rows 116
                         // (102), the shared prefix 62 (58), listed pages 140 (131).
                         f2 sum[2] = {0ull, 0ull};
-                            const f2 sc2 = mk2(sc, sc), rf2 = mk2(-ref, -ref);
+                            const float scm = fabsf(m) >= AP_HUGE / 4 ? 0.25f : sc;
+                            const f2 sc2 = mk2(scm, scm), rf2 = mk2(-ref, -ref);
 #pragma unroll 1
                             for (int c = 0; c < KEYS / 32; ++c) {
                                 scores(c);

@@ -5,6 +5,8 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+from oracle import pages as op  # noqa: E402
+
 BF, F32 = torch.bfloat16, torch.float32
 
 
@@ -37,3 +39,32 @@ def test_infinite_values_that_every_row_sees(dtype, lists):
         assert (got[b, :n[b], 4 * h:4 * h + 4, d] == x).all(), (b, h, d)
         got[b, :n[b], 4 * h:4 * h + 4, d] = 0
     assert np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("length", [200, 60000])      # one part, several
+def test_scores_of_any_size(length, sign, dtype):
+    """Keys along one channel: scores are one product, exact, and equal ones weigh the same however large."""
+    import kv8_cases as kc
+    import pages_cases as pc
+    sizes = [0, 3, 8, 12, 14, 15, 16, 17, 18, 20, 30, 50, 62]
+    B = len(sizes)
+    c = pc.Cache(kc.make_ctx(8, 2, 64), [length] * B, 3)
+    q = torch.zeros((B, 1, 8, 64), dtype=dtype, device="cuda")
+    c.k.nan_to_num_(0.0).zero_()
+    alike = np.arange(5, length, 7)
+    for b, e in enumerate(sizes):
+        x = sign * 1.375 * 2.0 ** e
+        q[b, :, :, 0] = 1.625 * 2.0 ** e
+        rows = torch.from_numpy(c.tab[b, :-(-length // 16)].astype(np.int64)).cuda()
+        key = torch.full((len(rows) * 16,), x * (0.5 if sign > 0 else 2), device="cuda").to(BF)   # below the largest
+        key[torch.from_numpy(alike).cuda()] = x
+        c.k[0, rows, :, :, 0] = key.view(-1, 1, 16).expand(-1, 2, -1)
+    out = pc.attend(c, [1] * B, q)
+    assert int(c.status.item()) == 0
+    for b, e in enumerate(sizes):
+        o, spread, size = op.attend(pc.dbl(q[b]), pc.Cache.rows(c, b, c.k), pc.Cache.rows(c, b, c.v), np.ones((1, 2, length), bool))
+        # products are exact; from 2^8 on the others are 2^11 and more below, and weigh nothing
+        far = np.abs(pc.dbl(out[b]) - o) - pc.tolerance(dtype, o, spread, size if e < 8 else 0)
+        assert (far <= 0).all(), (e, far.max())

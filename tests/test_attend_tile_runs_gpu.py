@@ -64,3 +64,37 @@ def test_listed_pages_around_runs(dtype):
     assert int(c.status.item()) == 0
     which = [0, 1, 2, 3, 45, 89]
     pc.check(c.some(which), out[which], [1] * 6, q[which], pages=pages[which])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_runs_without_a_finite_score_and_values_that_are_not_finite(dtype):
+    """A first run of scores of -inf (float32 queries: -4e36, their planes give NaN for an infinite key) leaves
+    nothing behind; a value that is not finite in one of several runs, and the largest score in the last of them."""
+    import pages_cases as pc
+    from oracle import pages as op
+    B, T = 200, 36000
+    c = _Alike(8, 2, 64, [T] * B, 3)
+    q = pc.queries(c.ctx, B, 1, dtype, 4).contiguous()
+    page = lambda t: torch.from_numpy(c.tab[0, t // 16].astype(np.int64)).cuda()  # noqa: E731
+    early = np.arange(0, 17008, 16)
+    q[..., 0] = 1
+    c.k[0, page(early), 0, :, 0] = float("-inf") if dtype == BF else -3e37                # KV head 0: 17008 keys
+    c.v[0, int(c.tab[0, 20000 // 16]), 1, 20000 % 16, 5] = float("inf")   # KV head 1: one value, and a key like the query
+    last = (35000 // 16, 35000 % 16)
+    c.k[0, int(c.tab[0, last[0]]), 1, last[1]] = 2.0
+    q[:, :, 4:] = q[:, :, 4:].abs()
+    out = pc.attend(c, [1] * B, q)
+    assert int(c.status.item()) == 0
+    for b in (0, 7, 101, 199):
+        k, v, x = pc.Cache.rows(c, b, c.k), pc.Cache.rows(c, b, c.v), pc.dbl(q[b])
+        see = np.ones((1, 2, T), bool)
+        see[:, 0, :17008] = False
+        inf = np.isinf(v[:, 1, 5])
+        assert inf.sum() == 1
+        v[inf, 1, 5] = 0
+        k[:17008, 0, 0] = 0                                             # (not seen there)
+        o, spread, size = op.attend(x, k, v, see)
+        got = pc.dbl(out[b])
+        assert (got[0, 4:, 5] == np.inf).all()
+        got[0, 4:, 5], spread[0, 4:, 5] = o[0, 4:, 5], 1
+        assert (np.abs(got - o) <= pc.tolerance(dtype, o, spread, size)).all(), b
