@@ -1003,7 +1003,7 @@ __global__ void __launch_bounds__(C::THREADS, 1)
             const ApRing rg = ring_of(two, s);
             Walk k = begin(two, s);
             ApSlot vs{1, 0};
-            while (next(k)) {
+            while (go && next(k)) {
                 const ApUnit &u = k.u;
                 const int q0 = u.i0 + (two ? s * C::QR : 0), nq = two && s ? u.nq - C::QR : min(u.nq, C::QR);   // the stream's queries
                 // ------------------------------------------------ queries
